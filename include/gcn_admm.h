@@ -180,6 +180,50 @@ int gcn_admm_dense_product(gcn_admm* h, const float* A, const float* B, float* C
 int gcn_admm_dense_product_tn(gcn_admm* h, const float* A, const float* B, float* C, long long rows, int ka, int nb,
                               int tensor_cores);
 
+/* ---- products grouped by expert, and the update of such weights --------------------------------------------------------
+ * (No counterpart in the paper: the products of Problem 1 and of the block updates, for programs that give every group of rows a
+ * weight of its own -- a weight per community of Section 2, or the experts of a layer whose rows were sorted by expert.)
+ * Matrices are row-major on the handle's device, of `type`:
+ *  GCN_ADMM_F32   products to fp32 accuracy: operands as sums of three bf16 numbers (24 bits, the exponents of fp32)
+ *  GCN_ADMM_BF16, GCN_ADMM_F16   products exact, sums in fp32
+ * Sums are rounded once, to out_type: the type of the operands, or GCN_ADMM_F32.  Leading dimensions and strides between matrices count
+ * elements; 0 means dense.  Any alignment to whole elements and any sizes will do; 16-bit matrices whose address, leading dimension
+ * and stride are multiples of 16 bytes are read fastest.  Infinite or NaN elements leave every result non-finite that the
+ * formula has them in, though not always the same infinity or NaN; other results are untouched by them.
+ * Group g owns the rows offsets[g] <= i < offsets[g+1], 0 <= g < n_groups <= 1024, cut to 0..rows; where offsets descend it
+ * owns none.  offsets: device array of n_groups + 1 ints, read when the work runs, so that a router on the device may write them.  NULL: the
+ * handle's communities, in the order of gcn_admm_index (n_groups and rows must then be the handle's).  Groups should not overlap (rows of two
+ * groups get one of the two results).  Results may not alias operands.
+ * All work is enqueued on the handle's stream; the calls return without synchronising, may be captured, and give the same bits
+ * every time.  gcn_admm_grouped_product_tn and gcn_admm_orthogonalise use a workspace of the handle that grows when a call needs more
+ * of it: the first call of a size allocates and may not be part of a capture.  Calls, and replays of captured ones, that share a handle must
+ * follow one another on its stream.  A bounded wait that runs out on the device is reported like that of any product (see
+ * GCN_ADMM_ST_PIPELINE_FLAG). */
+enum { GCN_ADMM_F32 = 0, GCN_ADMM_BF16 = 1, GCN_ADMM_F16 = 2 };
+
+/* y[i] = x[i] W_g for the rows i of every group g; rows that no group owns are left as they are.  x: rows x k, y: rows x n.
+ * transpose_w 0: W_g is the k x n matrix at w + g stride_w; 1: it is the transpose of the n x k matrix there.  The gradient of x is the same call
+ * with y's gradient for x, k and n exchanged, the same w, and transpose_w the other way round. */
+int gcn_admm_grouped_product(gcn_admm* h, int type, const void* x, long long ldx, const void* w, long long ldw, long long stride_w,
+                             int transpose_w, const int* offsets, int n_groups, long long rows, int k, int n, int out_type, void* y,
+                             long long ldy);
+
+/* dw_g = sum over the rows i of group g of x[i]^T y[i]: the gradient of W_g where y is that of the product.  x: rows x ka, y: rows x nb,
+ * dw_g: ka x nb at dw + g stride_dw, zero for a group without rows. */
+int gcn_admm_grouped_product_tn(gcn_admm* h, int type, const void* x, long long ldx, const void* y, long long ldy, const int* offsets,
+                                int n_groups, long long rows, int ka, int nb, int out_type, void* dw, long long lddw,
+                                long long stride_dw);
+
+/* An update of weights turned towards the nearest matrix with orthonormal rows (or columns), by Newton-Schulz products: for each of the
+ * `batch` matrices G, rows x cols, X_0 = G / (||G||_F + eps) and n_steps times X <- a X + (b A + c A A) X with A = X X^T (X^T in place
+ * of X where rows > cols); out = scale X.  coefficients: a, b, c of every step, host array of 3 n_steps floats.  Each singular value s
+ * goes to s (a + b s^2 + c s^4); coefficients that let one grow above 16, or a factor a + b s^2 + c s^4 above 1024, are refused.  A
+ * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  All products to fp32 accuracy, whatever the type, by pairs of
+ * halves under fixed scales (the entries are bounded by the singular values).  out may be g itself. */
+int gcn_admm_orthogonalise(gcn_admm* h, int type, int batch, int rows, int cols, const void* g, long long ldg, long long stride_g,
+                           int n_steps, const float* coefficients, float eps, float scale, int out_type, void* out, long long ldo,
+                           long long stride_o);
+
 /* ---- propagation for callers that cannot allocate ---------------------------------------------
  * (No counterpart in the paper: this is a packaging variant of gcn_admm_propagate.)
  * Same result as gcn_admm_propagate, for code that is not allowed to reserve device memory when it

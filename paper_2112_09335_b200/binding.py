@@ -19,13 +19,14 @@ EXPORTS = [
     "gcn_admm_predict", "gcn_admm_destroy", "gcn_admm_release_idle", "gcn_admm_last_error", "gcn_admm_propagate", "gcn_admm_index",
     "gcn_admm_get_state", "gcn_admm_set_state", "gcn_admm_step_block", "gcn_admm_decisions",
     "gcn_admm_launches", "gcn_admm_profile", "gcn_admm_profile_read", "gcn_admm_propagate_static", "gcn_admm_dense_product", "gcn_admm_dense_product_tn",
-    "gcn_admm_shard_plan", "gcn_admm_propagate_sharded",
+    "gcn_admm_shard_plan", "gcn_admm_propagate_sharded", "gcn_admm_grouped_product", "gcn_admm_grouped_product_tn", "gcn_admm_orthogonalise",
 ]
 
 IX = dict(perm=0, inv_perm=1, comm_ptr=2, nbr=3, halo1=4, halo2=5, csr_row_ptr=6, csr_col=7,
           seg_row_ptr=8, seg_comm=9, seg_begin=10)
 ST_W, ST_Z, ST_U, ST_TAU, ST_THETA, ST_PIPELINE_FLAG = range(6)
 PHASE_W, PHASE_Z, PHASE_U = range(3)
+F32, BF16, F16 = range(3)
 
 
 class Params(C.Structure):
@@ -72,6 +73,9 @@ def load():
     lib.gcn_admm_propagate_sharded.argtypes = [vp, i32, vp, i32, vp, C.POINTER(i64)]
     lib.gcn_admm_dense_product.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32]
     lib.gcn_admm_dense_product_tn.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32]
+    lib.gcn_admm_grouped_product.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, vp, i32, i64, i32, i32, i32, vp, i64]
+    lib.gcn_admm_grouped_product_tn.argtypes = [vp, i32, vp, i64, vp, i64, vp, i32, i64, i32, i32, i32, vp, i64, i64]
+    lib.gcn_admm_orthogonalise.argtypes = [vp, i32, i32, i32, i32, vp, i64, i64, i32, vp, C.c_float, C.c_float, i32, vp, i64, i64]
     lib.gcn_admm_index.argtypes = [vp, i32, i32, C.POINTER(C.POINTER(i32)), C.POINTER(i64)]
     lib.gcn_admm_shard_plan.argtypes = [vp, i32, i32, i32, i32, C.POINTER(C.POINTER(i32)), C.POINTER(i64)]
     lib.gcn_admm_get_state.argtypes = [vp, i32, i32, vp]
@@ -92,6 +96,11 @@ def _ptr(a):
     if isinstance(a, int):
         return C.c_void_p(a)
     return a.ctypes.data_as(C.c_void_p)
+
+
+def _dev(address):
+    """A device address; None and 0 (an empty tensor's) are NULL."""
+    return _ptr(int(address)) if address else None
 
 
 def default_params() -> Params:
@@ -205,6 +214,29 @@ class GcnAdmm:
         """C = A^T B between dense device buffers (addresses as ints): A rows x ka, B rows x nb."""
         self._check(self._lib.gcn_admm_dense_product_tn(self._h, _ptr(int(a_dev)), _ptr(int(b_dev)), _ptr(int(c_dev)),
                                                         int(rows), int(ka), int(nb), int(tensor_cores)))
+
+    def grouped_product(self, x_dev, w_dev, y_dev, offsets_dev, n_groups, rows, k, n, type=F32, out_type=None, transpose_w=False, ldx=0, ldw=0,
+                        stride_w=0, ldy=0):
+        """y[i] = x[i] W_g for the rows i of every group g, between device buffers (addresses as ints); ``offsets_dev`` None: the
+        handle's communities.  Strides in elements, 0: dense.  Enqueued on the handle's stream."""
+        self._check(self._lib.gcn_admm_grouped_product(self._h, int(type), _dev(x_dev), int(ldx), _dev(w_dev), int(ldw), int(stride_w), int(transpose_w),
+                                                       _dev(offsets_dev), int(n_groups), int(rows), int(k), int(n),
+                                                       int(type if out_type is None else out_type), _dev(y_dev), int(ldy)))
+
+    def grouped_product_tn(self, x_dev, y_dev, dw_dev, offsets_dev, n_groups, rows, ka, nb, type=F32, out_type=None, ldx=0, ldy=0, lddw=0, stride_dw=0):
+        """dw_g = sum over the rows i of group g of x[i]^T y[i], between device buffers (addresses as ints)."""
+        self._check(self._lib.gcn_admm_grouped_product_tn(self._h, int(type), _dev(x_dev), int(ldx), _dev(y_dev), int(ldy), _dev(offsets_dev),
+                                                          int(n_groups), int(rows), int(ka), int(nb), int(type if out_type is None else out_type),
+                                                          _dev(dw_dev), int(lddw), int(stride_dw)))
+
+    def orthogonalise(self, g_dev, out_dev, batch, rows, cols, coefficients, eps=1e-7, scale=1.0, type=F32, out_type=None, ldg=0, stride_g=0, ldo=0,
+                      stride_o=0):
+        """out = scale X after one step X <- a X + (b A + c A A) X, A = X X^T, for every (a, b, c) of ``coefficients``, from
+        X = G / (||G|| + eps), for every matrix of a batch, between device buffers (addresses as ints)."""
+        co = np.ascontiguousarray(coefficients, dtype=np.float32).reshape(-1, 3)
+        self._check(self._lib.gcn_admm_orthogonalise(self._h, int(type), int(batch), int(rows), int(cols), _dev(g_dev), int(ldg), int(stride_g), len(co),
+                                                     _ptr(co), float(eps), float(scale), int(type if out_type is None else out_type), _dev(out_dev),
+                                                     int(ldo), int(stride_o)))
 
     def index(self, which, comm=0):
         data = C.POINTER(C.c_int)()

@@ -5,8 +5,9 @@ import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(HERE, "csrc", "gcn_admm.cu")]
+SOURCES = [os.path.join(HERE, "csrc", "gcn_admm.cu"), os.path.join(HERE, "csrc", "grouped.cu")]
 HEADERS = [os.path.join(HERE, "csrc", "kernels.cuh"), os.path.join(HERE, "csrc", "gemm_half.cuh"), os.path.join(HERE, "csrc", "gemm_tc.cuh"), os.path.join(HERE, "csrc", "graph_index.hpp"), os.path.join(HERE, "csrc", "shard_plan.hpp"), os.path.join(HERE, "csrc", "memory.hpp"),
+           os.path.join(HERE, "csrc", "grouped.hpp"), os.path.join(HERE, "csrc", "grouped_plan.hpp"),
            os.path.join(os.path.dirname(HERE), "include", "gcn_admm.h")]
 LIB = os.path.join(HERE, "libgcn_admm.so")
 
@@ -30,7 +31,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     cmd = [nvcc_path(), "-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC,-fopenmp", "-shared"]
+           "-Xcompiler", "-fPIC,-fopenmp", "-shared", "-t", "0"]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += SOURCES + ["-o", LIB]

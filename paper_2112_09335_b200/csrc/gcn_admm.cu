@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <new>
@@ -20,6 +21,7 @@
 #include "gemm_half.cuh"
 #include "gemm_tc.cuh"
 #include "graph_index.hpp"
+#include "grouped.hpp"
 #include "kernels.cuh"
 #include "memory.hpp"
 #include "shard_plan.hpp"
@@ -227,6 +229,10 @@ struct gcn_admm {
   float* item_sums = nullptr;             // n_items x max_ld
   size_t item_sums_elems = 0;
   gcn_admm_mem::Slab wide_sums;           // the same for the widest matrix gcn_admm_propagate was given, where that is wider than every layer
+  int* d_comm_ptr = nullptr;              // [M+1] rows of the communities: the groups of a grouped product that names none
+  gcn_admm_mem::Slab work;                // workspace of the grouped products and orthogonalised updates, counters of finished tiles first
+  size_t work_tickets = 0;                // how many
+  std::vector<gcn_admm_mem::Slab> old_work;   // what it was before it grew: graphs that the caller captured still use it
   unsigned char* d_train = nullptr;
   int* d_train_rows = nullptr;            // new ids of the training rows, ascending
   float* d_fista_momentum = nullptr;      // (t_j - 1) / t_{j+1}, j = 1..fista_iters
@@ -396,6 +402,37 @@ struct gcn_admm {
     gcn_admm_mem::Pool::get().give(wide_sums);
     wide_sums = gcn_admm_mem::Slab{};
     wide_sums = take_slab(need * sizeof(float));
+  }
+
+  // Workspace for a call that needs `bytes` beside `tickets` counters.  It only grows, and what it has outgrown stays until the handle ends.
+  gcn_admm_grouped::Room room_for(size_t bytes, size_t tickets) {
+    using gcn_admm_grouped::Room;
+    const auto behind = [](size_t count) { return (count * sizeof(unsigned) + 1023) / 1024 * 1024; };
+    if (tickets > work_tickets || (bytes > 0 && behind(work_tickets) + bytes > work.size)) {
+      cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+      CU(cudaStreamIsCapturing(stream, &capture));
+      if (capture != cudaStreamCaptureStatusNone)
+        throw Fail{GCN_ADMM_ERR_ARG, "the workspace would have to grow, which a stream that is being captured does not allow: make the call once before"};
+      const size_t count = std::max(tickets, work_tickets);
+      old_work.reserve(old_work.size() + 1);
+      gcn_admm_mem::Slab larger = take_slab(behind(count) + std::max(bytes, work.size - std::min(work.size, behind(work_tickets))));
+      if (work.base) old_work.push_back(work);
+      work = larger;
+      work_tickets = count;
+      CU(cudaMemsetAsync(work.base, 0, behind(count), stream));
+    }
+    return Room{work.base + behind(work_tickets), reinterpret_cast<unsigned*>(work.base), tc_error, stream, &launches};
+  }
+  // Refuses pointers that kernels on this handle's device cannot follow.
+  void need_device(std::initializer_list<const void*> pointers) const {
+    for (const void* q : pointers) {
+      if (q == nullptr) continue;
+      cudaPointerAttributes a;
+      const bool known = cudaPointerGetAttributes(&a, q) == cudaSuccess;
+      if (!known) cudaGetLastError();
+      if (!known || !(a.type == cudaMemoryTypeManaged || (a.type == cudaMemoryTypeDevice && a.device == p.device)))
+        throw Fail{GCN_ADMM_ERR_ARG, "matrices and offsets must lie on the handle's device"};
+    }
   }
 
   template <typename T> struct Same { using type = T; };   // keeps a parameter out of template deduction
@@ -1106,6 +1143,7 @@ struct gcn_admm {
       CU(cudaMemsetAsync(&report->error, 0, sizeof(int), stream));
       CU(cudaMemsetAsync(&report->status, 0, sizeof(int), stream));   // decisions since then may have read anything
       for (const auto& c : counters) CU(cudaMemsetAsync(*c.first, 0, c.second, stream));
+      if (work_tickets > 0) CU(cudaMemsetAsync(work.base, 0, work_tickets * sizeof(unsigned), stream));
       fresh = false;
       throw Fail{GCN_ADMM_ERR_CUDA, r.error & gk::kErrGridBarrier ? "a step-size search gave up waiting for the rest of its grid"
                                                                   : "a tensor-core product gave up waiting on its pipeline"};
@@ -1307,6 +1345,7 @@ void create_impl(gcn_admm* h, long long n, const long long* row_ptr, const int* 
   h->want_table(h->d_perm, g.perm);
   h->want_table(h->d_inv, g.inv);
   h->want_table(h->d_dinv, g.dinv);
+  h->want_table(h->d_comm_ptr, g.comm_ptr);
   h->want_table(h->d_col_comm, g.col_comm);
   h->want_table(h->d_y, y_new);
   h->want_table(h->d_train, t_new);
@@ -1619,7 +1658,8 @@ void gcn_admm_destroy(gcn_admm* h) {
     for (cudaEvent_t e : {h->side.begun, h->side.w_done, h->side.out_done, h->side.done})
       if (e) cudaEventDestroy(e);
     for (cudaEvent_t e : h->event_pool) cudaEventDestroy(e);
-    for (const gcn_admm_mem::Slab& q : {h->slab, h->wide_sums}) gcn_admm_mem::Pool::get().give(q);
+    for (const gcn_admm_mem::Slab& q : {h->slab, h->wide_sums, h->work}) gcn_admm_mem::Pool::get().give(q);
+    for (const gcn_admm_mem::Slab& q : h->old_work) gcn_admm_mem::Pool::get().give(q);
     h->stage.close();
   }
   cudaGetLastError();
@@ -1897,6 +1937,67 @@ int gcn_admm_dense_product_tn(gcn_admm* h, const float* A, const float* B, float
     }
     cudaFree(a); cudaFree(b); cudaFree(c);
     h->check_status();
+  });
+}
+
+// ---- products grouped by expert, orthogonalised updates -------------------------------------------
+namespace {
+// The caller's offsets, or those of the handle's communities where none are given.
+const int* offsets_or_communities(gcn_admm* h, const int* offsets, int n_groups, long long rows) {
+  if (offsets != nullptr) {
+    if (reinterpret_cast<uintptr_t>(offsets) % sizeof(int) != 0) throw Fail{GCN_ADMM_ERR_ARG, "offsets are not aligned to their elements"};
+    return offsets;
+  }
+  if (n_groups != h->M || rows != h->n) throw Fail{GCN_ADMM_ERR_ARG, "without offsets the groups are the handle's communities: n_groups and rows must be theirs"};
+  return h->d_comm_ptr;
+}
+}  // namespace
+
+int gcn_admm_grouped_product(gcn_admm* h, int type, const void* x, long long ldx, const void* w, long long ldw, long long stride_w, int transpose_w,
+                             const int* offsets, int n_groups, long long rows, int k, int n, int out_type, void* y, long long ldy) {
+  return guarded(h, [&] {
+    gcn_admm_grouped::Product p{type, out_type, x, ldx, w, ldw, stride_w, transpose_w != 0, offsets, n_groups, rows, k, n, y, ldy};
+    if (const char* const wrong = gcn_admm_grouped::check(p)) throw Fail{GCN_ADMM_ERR_ARG, wrong};
+    p.offsets = offsets_or_communities(h, offsets, n_groups, rows);
+    if (rows == 0) return;
+    h->need_device({x, w, y, offsets});
+    char name[48];
+    std::snprintf(name, sizeof name, "grouped@%dx%d", k, n);
+    const int size = gcn_admm_grouped::size_of(type);
+    gcn_admm::Scope sc(h, name, 0, (double)rows * k * size + (double)n_groups * k * n * size + (double)rows * n * gcn_admm_grouped::size_of(out_type), 2.0 * (double)rows * k * n);
+    CU(gcn_admm_grouped::enqueue(p, gcn_admm_grouped::Room{nullptr, nullptr, h->tc_error, h->stream, &h->launches}));
+  });
+}
+
+int gcn_admm_grouped_product_tn(gcn_admm* h, int type, const void* x, long long ldx, const void* y, long long ldy, const int* offsets, int n_groups,
+                                long long rows, int ka, int nb, int out_type, void* dw, long long lddw, long long stride_dw) {
+  return guarded(h, [&] {
+    gcn_admm_grouped::ProductTn p{type, out_type, x, ldx, y, ldy, offsets, n_groups, rows, ka, nb, dw, lddw, stride_dw};
+    if (const char* const wrong = gcn_admm_grouped::check(p)) throw Fail{GCN_ADMM_ERR_ARG, wrong};
+    p.offsets = offsets_or_communities(h, offsets, n_groups, rows);
+    h->need_device({rows > 0 ? x : nullptr, rows > 0 ? y : nullptr, dw, offsets});
+    const gcn_admm_grouped::Room room = h->room_for(gcn_admm_grouped::space_bytes(p), gcn_admm_grouped::tickets_of(p));
+    char name[48];
+    std::snprintf(name, sizeof name, "grouped_tn@%dx%d", ka, nb);
+    gcn_admm::Scope sc(h, name, 0, (double)rows * (ka + nb) * gcn_admm_grouped::size_of(type) + (double)n_groups * ka * nb * gcn_admm_grouped::size_of(out_type),
+                       2.0 * (double)rows * ka * nb);
+    CU(gcn_admm_grouped::enqueue(p, room));
+  });
+}
+
+int gcn_admm_orthogonalise(gcn_admm* h, int type, int batch, int rows, int cols, const void* g, long long ldg, long long stride_g, int n_steps,
+                           const float* coefficients, float eps, float scale, int out_type, void* out, long long ldo, long long stride_o) {
+  return guarded(h, [&] {
+    gcn_admm_grouped::Orthogonal p{type, out_type, batch, rows, cols, g, ldg, stride_g, n_steps, coefficients, eps, scale, out, ldo, stride_o};
+    if (const char* const wrong = gcn_admm_grouped::check(p)) throw Fail{GCN_ADMM_ERR_ARG, wrong};
+    h->need_device({g, out});
+    const gcn_admm_grouped::Room room = h->room_for(gcn_admm_grouped::space_bytes(p), 0);
+    char name[48];
+    std::snprintf(name, sizeof name, "orthogonalise@%dx%d", rows, cols);
+    const double m = std::min(rows, cols), w = std::max(rows, cols);
+    gcn_admm::Scope sc(h, name, 0, (double)batch * m * w * (gcn_admm_grouped::size_of(type) + gcn_admm_grouped::size_of(out_type)),
+                       (double)batch * n_steps * (m * (m + 1) * w + m * (m + 1) * m + 2 * m * m * w));
+    CU(gcn_admm_grouped::enqueue(p, room));
   });
 }
 
