@@ -25,7 +25,10 @@
 #include "kernels.cuh"
 #include "memory.hpp"
 #include "shard_plan.hpp"
+#include "tensor_map.hpp"
 
+using gcn_admm_host::encode_tiled;
+using gcn_admm_host::EncodeTiledFn;
 using gcn_admm_host::GraphIndex;
 
 namespace {
@@ -97,23 +100,6 @@ T* dalloc(size_t count) {
     throw Fail{e == cudaErrorMemoryAllocation ? GCN_ADMM_ERR_ALLOC : GCN_ADMM_ERR_CUDA,
                std::string("cudaMalloc: ") + cudaGetErrorString(e)};
   return static_cast<T*>(p);
-}
-
-// cuTensorMapEncodeTiled, looked up through the runtime (the library does not link the driver API directly).
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled() {
-  static EncodeTiledFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      p = nullptr;
-    }
-    return reinterpret_cast<EncodeTiledFn>(p);
-  }();
-  return fn;
 }
 
 // Tensor map of a row-major rows x ld fp32 matrix for 128-row x 32-column tiles written with the 128-byte

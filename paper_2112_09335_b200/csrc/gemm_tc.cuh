@@ -180,11 +180,11 @@ __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity) {
 }
 // Copies: `started` of them, number i reporting to barrier i mod `slots` (a stage some producer never filled has no such end:
 // the bound covers it).  By one thread.
-__device__ __noinline__ void drain_copies(uint32_t bars, int slots, int started) {
+static __device__ __noinline__ void drain_copies(uint32_t bars, int slots, int started) {
   for (int i = max(0, started - slots); i < started; ++i) drain_wait(bars + 8 * (i % slots), (uint32_t)(i / slots) & 1u);
 }
 // MMAs: by the thread that issued them, on a barrier nothing else uses.
-__device__ __noinline__ void drain_mmas(uint32_t bar) {
+static __device__ __noinline__ void drain_mmas(uint32_t bar) {
   mma_commit(bar);
   drain_wait(bar, 0);
 }

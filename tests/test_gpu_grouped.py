@@ -1,10 +1,10 @@
 """Products grouped by expert, both gradients, and orthogonalised updates against plain fp64 implementations.
 
 Tolerances.  An output of type t is off by half a step, eps(t) / 2 of its value, from rounding, and before that by the sum's error.  Operands
-are exact (16 bits) or held to 2^-24 of their magnitude in three parts whose left-out products are below 2^-24 in all.  Sums are formed in pieces of at
+are exact, in one part of 16 bits or three of 8 bits each, whose left-out products are below 2^-21 in all.  Sums are formed in pieces of at
 most 256 products in fp32 (16 matrix instructions whose accumulator is cut toward zero, 2^-23 of the sum of magnitudes each, their internal
-alignment as much again), which are added in fp32.  So |error| <= eps(t)/2 |y| + (2 * 16 + 8 + K / 256) 2^-23 sum |a||b|.  Where tokens of
-a whole test are compared in the 2-norm, the same counts against the norm of y for operands of random sign, whose partial sums are no larger.
+alignment as much again), which are added in fp32.  So |error| <= eps(t)/2 |y| + (2 * 16 + 8 + K / 256) 2^-23 sum |a||b|.  Where
+a whole result is compared in the 2-norm, the same counts against the norm of y for operands of random sign, whose partial sums are no larger.
 """
 import numpy as np
 import pytest
