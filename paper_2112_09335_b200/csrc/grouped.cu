@@ -17,34 +17,6 @@ __device__ __forceinline__ void put(float* at, float x) { *at = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* at, float x) { *at = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void put(__half* at, float x) { *at = __float2half_rn(x); }
 
-constexpr int kTile = 64, kStep = 16;
-
-// One 64 x 64 tile of sum over c < K of a(i, c) b(c, j), by 256 threads of 4 x 4 elements.  `a` and `b` give an element, zero outside.
-template <typename GetA, typename GetB, typename Put>
-__device__ void tile_product(int K, const GetA& a, const GetB& b, const Put& put_at) {
-  __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  float acc[4][4] = {};
-  for (int c0 = 0; c0 < K; c0 += kStep) {
-    for (int e = tid; e < kStep * kTile; e += 256) {
-      sa[e & 15][e >> 4] = c0 + (e & 15) < K ? a(e >> 4, c0 + (e & 15)) : 0.f;
-      sb[e >> 6][e & 63] = c0 + (e >> 6) < K ? b(c0 + (e >> 6), e & 63) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < kStep; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[c][ty + 16 * i], sb[c][tx + 16 * j], acc[i][j]);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) put_at(ty + 16 * i, tx + 16 * j, acc[i][j]);
-}
-
 // ---- groups of rows ----------------------------------------------------------------------------------
 // Rows of a group: offsets[g] .. offsets[g+1] cut to 0 .. rows, none where they descend.  Whatever the offsets hold, no row outside of
 // the matrices is touched.  Offsets are read as they are when the kernel runs.
@@ -104,7 +76,7 @@ template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA>
 struct ProductJob {
   using T = T_;
   using Args = ProductArgs;
-  static constexpr int kParts = PARTS, kBN = BN;
+  static constexpr int kParts = PARTS, kBN = BN, kSegment = 4;
   static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kMeets = false;
   struct Item {
     int chunks, n, tail, g, row0, left, col0;
@@ -197,7 +169,7 @@ template <typename T_, int PARTS, int BN, bool TMA>
 struct ProductTnJob {
   using T = T_;
   using Args = ProductTnArgs;
-  static constexpr int kParts = PARTS, kBN = BN;
+  static constexpr int kParts = PARTS, kBN = BN, kSegment = 4;
   static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kMeets = true;
   struct Item {
     int chunks, n, tail, g, row0, end, m0, col0;
@@ -319,49 +291,240 @@ struct ProductTnJob {
   }
 };
 
-// X = G / (||G|| + eps), a block for every matrix; rows are the shorter side.  The norm is summed in fp64: squares of fp32 numbers leave
-// the range of fp32.
+// ---- orthogonalised updates --------------------------------------------------------------------------
+// X <- P X with P = a I + b S + c S S, S = X X^T; for matrices taller than wide X <- X P with S = X^T X.  Three products a step, all by pairs
+// of halves (three matrix instructions for one, 22 bits of each operand): single halves, at 11 bits, end 1e-3 off, more than a bf16 result may lose, and
+// 4e-2 where singular values span four decades, since the steps lift the small ones, and what they are off, by |a| each.
+// Matrices between products are images: part hi of all matrices, then part lo, rows padded to 16 bytes, under a power of two that comes from
+// the bounds of the singular values (host, grow()): entries stay below 2^15 and far above the smallest half.  S and P are symmetric: only
+// tiles that reach the diagonal are formed, the others are written turned.  X keeps its own orientation throughout, so nothing is transposed.
+struct Image {
+  __half* at;
+  int rows, ld;            // ld: columns rounded up to 8
+  long long part;          // from hi to lo
+  __device__ __forceinline__ __half* matrix(int b) const { return at + (long long)b * rows * ld; }
+};
+
+constexpr int kNormBlocks = 64;   // partial sums of a norm, at most
+
+// Partial sums of squares of every matrix; in fp64: squares of fp32 numbers leave the range of fp32.
 template <typename T>
-__global__ void __launch_bounds__(256) k_normalise(const Orthogonal p, float* __restrict__ x, int m, int n) {
-  __shared__ double s_sum[256];
-  const bool turn = p.rows > p.cols;
-  const T* const g = static_cast<const T*>(p.g) + blockIdx.x * p.stride_g;
-  const auto at = [&](long long e) { return (double)to_float(turn ? g[(e % n) * p.ldg + e / n] : g[(e / n) * p.ldg + e % n]); };
+__global__ void __launch_bounds__(256) k_norm(const Orthogonal p, double* __restrict__ partial) {
+  gtc::enter_kernel();
+  __shared__ double s_sum[8];
+  const T* const g = static_cast<const T*>(p.g) + (long long)blockIdx.y * p.stride_g;
+  const unsigned cols = p.cols, count = (unsigned)p.rows * cols;
   double sum = 0.0;
-  for (long long e = threadIdx.x; e < (long long)m * n; e += 256) sum += at(e) * at(e);
-  s_sum[threadIdx.x] = sum;
-  __syncthreads();
-  for (int d = 128; d > 0; d >>= 1) {
-    if (threadIdx.x < d) s_sum[threadIdx.x] += s_sum[threadIdx.x + d];
-    __syncthreads();
+  for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += gridDim.x * 256) {
+    const unsigned row = e / cols;
+    const double x = (double)to_float(g[row * p.ldg + (e - row * cols)]);
+    sum = fma(x, x, sum);
   }
-  const double norm = sqrt(s_sum[0]) + (double)p.eps, inverse = norm > 0.0 ? 1.0 / norm : 0.0;
-  for (long long e = threadIdx.x; e < (long long)m * n; e += 256) x[(long long)blockIdx.x * m * n + e] = (float)(at(e) * inverse);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) sum += s_sum[w];
+    partial[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
+  }
 }
 
-// C = A B (B transposed where `bt`), matrices of a batch one after the other; where `d` is given, C = a I + b D + c A B.
-__global__ void __launch_bounds__(256) k_batch_product(const float* A, const float* B, float* C, int m, int n, int k, bool bt, const float* D, float a, float b, float c) {
-  const long long z = blockIdx.z;
-  A += z * m * k; B += z * n * k; C += z * m * n;
-  if (D != nullptr) D += z * m * n;
-  const int i0 = blockIdx.x * kTile, j0 = blockIdx.y * kTile;
-  tile_product(
-      k, [&](int i, int q) { return i0 + i < m ? A[(long long)(i0 + i) * k + q] : 0.f; },
-      [&](int q, int j) { return j0 + j < n ? bt ? B[(long long)(j0 + j) * k + q] : B[(long long)q * n + j0 + j] : 0.f; },
-      [&](int i, int j, float v) {
-        i += i0; j += j0;
-        if (i < m && j < n) C[(long long)i * n + j] = D != nullptr ? (i == j ? a : 0.f) + b * D[(long long)i * n + j] + c * v : v;
-      });
-}
-template <typename O>
-__global__ void __launch_bounds__(256) k_leave(const Orthogonal p, const float* __restrict__ x, int m, int n) {
-  const bool turn = p.rows > p.cols;
-  O* const out = static_cast<O*>(p.out) + blockIdx.z * p.stride_o;
-  for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < (long long)m * n; e += (long long)gridDim.x * 256) {
-    const long long i = e / n, j = e % n;
-    put(turn ? out + j * p.ldo + i : out + i * p.ldo + j, p.scale * x[(long long)blockIdx.z * m * n + e]);
+// X_0 = G / (||G|| + eps), to its image under `scale`; with no steps to take, `scale` times it, to the result.  A thread has eight elements of a row.
+template <typename T, typename O>
+__global__ void __launch_bounds__(256) k_start(const Orthogonal p, const double* __restrict__ partial, int partials, const Image x, float scale) {
+  gtc::enter_kernel();
+  __shared__ double s_inverse;
+  if (threadIdx.x == 0) {
+    double sum = 0.0;
+    for (int k = 0; k < partials; ++k) sum += partial[blockIdx.y * kNormBlocks + k];
+    const double norm = sqrt(sum) + (double)p.eps;
+    // a zero matrix stays zero, one that is not finite becomes NaN
+    s_inverse = !(norm > 0.0) ? (sum == 0.0 ? 0.0 : nan("")) : norm < INFINITY ? 1.0 / norm : nan("");
+  }
+  __syncthreads();
+  const double inverse = s_inverse;
+  const T* const g = static_cast<const T*>(p.g) + (long long)blockIdx.y * p.stride_g;
+  const unsigned units = x.ld / 8, count = (unsigned)p.rows * units;
+  for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += gridDim.x * 256) {
+    const unsigned row = e / units, col = (e - row * units) * 8;
+    const T* const src = g + row * p.ldg + col;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (int)col + k < p.cols ? (float)((double)to_float(src[k]) * inverse) * scale : 0.f;
+    if (x.at != nullptr) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+        const float2 f = __half22float2(h);
+        const __half2 l = __floats2half2_rn((v[2 * k] - f.x) * 0x1p11f, (v[2 * k + 1] - f.y) * 0x1p11f);
+        hi[k] = *reinterpret_cast<const uint32_t*>(&h);
+        lo[k] = *reinterpret_cast<const uint32_t*>(&l);
+      }
+      __half* const at = x.matrix(blockIdx.y) + (long long)row * x.ld + col;
+      *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(at + x.part) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    } else {
+      O* const at = static_cast<O*>(p.out) + (long long)blockIdx.y * p.stride_o + row * p.ldo + col;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if ((int)col + k < p.cols) put(at + k, v[k]);
+    }
   }
 }
+
+enum Stage { kGram, kPolynomial, kMove };
+struct OrthogonalArgs {
+  CUtensorMap a, b;
+  int* error_flag;
+  int batch, rows, cols, k;     // of the products: D is rows x cols, the reduction has k steps
+  float factor;                 // of the sums, for what is stored
+  float diagonal, linear;       // kPolynomial: a under the scale of P, b over the scale of S times that of P
+  Image s, to;                  // kPolynomial: S; where the result goes
+  void* out;                    // last kMove: the caller's matrix
+  int out_type;
+  long long ldo, stride_o;
+  bool vec_o;
+};
+
+// 32 rows x NC columns of halves as the NC rows x 32 columns of the turned matrix at `out`.
+template <int NC>
+__device__ __forceinline__ void store_turned(const float (&acc)[NC], uint8_t* buf, __half* out, long long ld, int rows_left, int cols_left) {
+  const int lane = threadIdx.x & 31, q = lane & 3;
+#pragma unroll
+  for (int c0 = 0; c0 < NC; c0 += 32) {
+    if (c0 < cols_left) {
+#pragma unroll
+      for (int c = 0; c < 32; ++c)
+        *reinterpret_cast<__half*>(buf + c * 64 + (((lane >> 3) ^ ((c >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2half_rn(acc[c0 + c]);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 8 * i + (lane >> 2), some = rows_left - 8 * q;
+        const uint4 v = *reinterpret_cast<const uint4*>(buf + c * 64 + ((q ^ ((c >> 1) & 3)) << 4));
+        __half* const at = out + (c0 + c) * ld + 8 * q;
+        if (c0 + c < cols_left && some > 0) {
+          if (some >= 8) {
+            *reinterpret_cast<uint4*>(at) = v;
+          } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e < some) reinterpret_cast<unsigned short*>(at)[e] = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
+          }
+        }
+      }
+      __syncwarp();
+    }
+  }
+}
+
+template <Stage STAGE, int BN, bool A_MN, bool B_MN>
+struct OrthogonalJob {
+  using Args = OrthogonalArgs;
+  static constexpr int kParts = 2, kBN = BN, kSegment = 1;
+  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kSymmetric = STAGE != kMove;
+  struct Item {
+    int chunks, n, tail, matrix, row0, col0;
+  };
+  const Args& a;
+  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*) : a(args) {}
+  __device__ __forceinline__ bool bf16() const { return false; }
+  __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
+  __device__ __forceinline__ void setup() {}
+  // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kBM / BN (i + 1)
+  __host__ __device__ static long long tiles(int rows, int cols) {
+    const long long m = (rows + kBM - 1) / kBM;
+    return kSymmetric ? kBM / BN * (m * (m + 1) / 2) : m * ((cols + BN - 1) / BN);
+  }
+  __device__ __forceinline__ bool item(unsigned i, Item& it) const {
+    const unsigned per = (unsigned)tiles(a.rows, a.cols);
+    it.matrix = (int)(i / per);
+    if (it.matrix >= a.batch) return false;
+    const unsigned t = i - (unsigned)it.matrix * per;
+    unsigned row, col;
+    if constexpr (kSymmetric) {
+      const unsigned u = t / (kBM / BN);   // in blocks of kBM columns
+      row = (unsigned)((sqrtf(8.f * (float)u + 1.f) - 1.f) * 0.5f);
+      while (row * (row + 1) / 2 > u) --row;
+      while ((row + 1) * (row + 2) / 2 <= u) ++row;
+      col = t - kBM / BN * (row * (row + 1) / 2);
+    } else {
+      const unsigned across = (unsigned)((a.cols + BN - 1) / BN);
+      row = t / across;
+      col = t - row * across;
+    }
+    it.row0 = (int)row * kBM;
+    it.col0 = (int)col * BN;
+    it.n = a.cols - it.col0;
+    it.chunks = it.n > 0 ? (a.k + kBK - 1) / kBK : 0;   // (a symmetric matrix's last row block may reach past its columns)
+    it.tail = kBK;
+    return true;
+  }
+  __device__ __forceinline__ void copy(const Item& it, int c, uint32_t tile, uint32_t bar) const {
+    constexpr int kBTile = BN * kBK * 2;
+    const int boxes_a = A_MN ? min(kBM / 64, (a.rows - it.row0 + 63) / 64) : kBM / 64, boxes_b = B_MN ? min(BN / 64, (it.n + 63) / 64) : BN / 64;
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)(2 * (boxes_a + boxes_b) * kGroup64)) : "memory");
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const int z = part * a.batch + it.matrix;
+      const uint32_t ta = tile + part * kATile, tb = tile + 2 * kATile + part * kBTile;
+      if constexpr (A_MN) {
+        for (int b = 0; b < boxes_a; ++b) copy_3d(ta + b * kGroup64, &a.a, it.row0 + 64 * b, c * kBK, z, bar);
+      } else {
+        copy_3d(ta, &a.a, c * kBK, it.row0, z, bar);
+      }
+      if constexpr (B_MN) {
+        for (int b = 0; b < boxes_b; ++b) copy_3d(tb + b * kGroup64, &a.b, it.col0 + 64 * b, c * kBK, z, bar);
+      } else {
+        copy_3d(tb, &a.b, c * kBK, it.col0, z, bar);
+      }
+    }
+  }
+  template <int NC>
+  __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], uint8_t* buf, int warp) const {
+    const int row0 = it.row0 + (warp & 3) * 32, col0 = it.col0 + (warp >> 2) * NC, row = row0 + (threadIdx.x & 31);
+    const int rows_left = a.rows - row0, cols_left = a.cols - col0;
+    if (rows_left <= 0 || cols_left <= 0) return;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] *= a.factor;
+    if constexpr (STAGE == kPolynomial) {
+      const __half* const s = a.s.matrix(it.matrix) + (long long)min(row, a.rows - 1) * a.s.ld + col0;
+#pragma unroll
+      for (int c0 = 0; c0 < NC; c0 += 8) {
+        if (c0 < cols_left) {   // rows of an image are padded to eight elements
+          const uint4 hi = *reinterpret_cast<const uint4*>(s + c0), lo = *reinterpret_cast<const uint4*>(s + a.s.part + c0);
+          const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
+            acc[c0 + 2 * e] = fmaf(a.linear, fmaf(y.x, 0x1p-11f, x.x), acc[c0 + 2 * e]);
+            acc[c0 + 2 * e + 1] = fmaf(a.linear, fmaf(y.y, 0x1p-11f, x.y), acc[c0 + 2 * e + 1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (row == col0 + c) acc[c] += a.diagonal;
+    }
+    if (STAGE == kMove && a.out != nullptr) {
+      const long long at = (long long)it.matrix * a.stride_o + row0 * a.ldo + col0;
+      void* const out = a.out_type == kF32 ? (void*)(static_cast<float*>(a.out) + at) : (void*)(static_cast<unsigned short*>(a.out) + at);
+      store_rows<NC>(acc, buf, out, a.ldo, a.out_type, a.vec_o, rows_left, cols_left);
+      return;
+    }
+    __half* const to = a.to.matrix(it.matrix);
+    const bool turn = kSymmetric && it.col0 + BN <= it.row0;
+    // images have room up to their leading dimension, and whole units there
+    store_rows<NC>(acc, buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
+    if (turn) store_turned<NC>(acc, buf, to + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = (acc[c] - __half2float(__float2half_rn(acc[c]))) * 0x1p11f;
+    store_rows<NC>(acc, buf, to + a.to.part + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
+    if (turn) store_turned<NC>(acc, buf, to + a.to.part + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+  }
+};
 
 template <typename F>
 void with_type(int type, const F& f) {
@@ -425,6 +588,26 @@ cudaError_t launch(const typename J::Args& args, unsigned grid, const Room& room
   return cudaLaunchKernelEx(&cfg, k_products<J>, args);
 }
 
+// The small kernels of 256 threads, launched the same way.
+template <typename... P, typename... Q>
+cudaError_t launch_plain(void (*kernel)(P...), dim3 grid, const Room& room, const Q&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(256);
+  cfg.stream = room.stream;
+  cudaLaunchAttribute behind{};
+  behind.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  behind.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &behind;
+  cfg.numAttrs = 1;
+  ++*room.launches;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+template <typename T>
+struct Tag {
+  using Type = T;
+};
+
 }  // namespace
 
 // Pieces of a weight gradient: the longest whose items give every SM one of about equal length.
@@ -448,10 +631,34 @@ std::size_t space_bytes(const ProductTn& p) {
   return (std::size_t)t.slots * kBM * t.bn * sizeof(float);
 }
 std::size_t tickets_of(const ProductTn& p) { return (std::size_t)plan(p).slots; }
-std::size_t space_bytes(const Orthogonal& p) {
-  const std::size_t m = std::min(p.rows, p.cols), n = std::max(p.rows, p.cols);
-  return (std::size_t)p.batch * (2 * m * n + 2 * m * m) * sizeof(float);
-}
+
+// The images of a call in its workspace.
+struct OrthogonalSpace {
+  double* partial;
+  Image x[2], s, p;
+  std::size_t bytes;
+  OrthogonalSpace(const Orthogonal& o, void* space) {
+    const int m = std::min(o.rows, o.cols);
+    std::size_t used = 0;
+    const auto take = [&](std::size_t size) {
+      void* const at = static_cast<char*>(space) + used;
+      used += (size + 255) / 256 * 256;
+      return at;
+    };
+    partial = static_cast<double*>(take((std::size_t)o.batch * kNormBlocks * sizeof(double)));
+    const auto image = [&](int rows, int cols) {
+      const int ld = (cols + 7) / 8 * 8;
+      const long long part = (long long)o.batch * rows * ld;
+      return Image{static_cast<__half*>(take(2 * part * sizeof(__half))), rows, ld, part};
+    };
+    x[0] = image(o.rows, o.cols);
+    x[1] = image(o.rows, o.cols);
+    s = image(m, m);
+    p = image(m, m);
+    bytes = used;
+  }
+};
+std::size_t space_bytes(const Orthogonal& p) { return OrthogonalSpace(p, nullptr).bytes; }
 
 cudaError_t enqueue(const Product& p, const Room& room) {
   if (p.rows == 0) return cudaSuccess;
@@ -521,23 +728,81 @@ cudaError_t enqueue(const ProductTn& p, const Room& room) {
 }
 
 cudaError_t enqueue(const Orthogonal& p, const Room& room) {
-  const int m = std::min(p.rows, p.cols), n = std::max(p.rows, p.cols);
-  float* x = static_cast<float*>(room.space);
-  float* y = x + (std::size_t)p.batch * m * n;
-  float *const s = y + (std::size_t)p.batch * m * n, *const f = s + (std::size_t)p.batch * m * m;
-  with_type(p.type, [&](auto in) { k_normalise<decltype(in)><<<p.batch, 256, 0, room.stream>>>(p, x, m, n); });
-  const dim3 square((unsigned)cdiv(m, kTile), (unsigned)cdiv(m, kTile), (unsigned)p.batch), wide((unsigned)cdiv(m, kTile), (unsigned)cdiv(n, kTile), (unsigned)p.batch);
-  for (int i = 0; i < p.steps; ++i) {
+  const int m = std::min(p.rows, p.cols);
+  const bool tall = p.rows > p.cols;
+  const OrthogonalSpace at(p, room.space);
+  const Image none{nullptr, p.rows, at.x[0].ld, 0};
+  // the power of two that keeps numbers up to `most` below 2^15
+  const auto scale_for = [](double most) { return std::ldexp(1.0, 14 - std::ilogb(most)); };
+  double most = 1.0, scale = p.steps > 0 ? scale_for(most) : (double)p.scale;
+  const long long elements = (long long)p.rows * p.cols;
+  const int partials = (int)std::min<long long>(kNormBlocks, cdiv(elements, 2048));
+  cudaError_t e = cudaSuccess;
+  with_type(p.type, [&](auto in) { e = launch_plain(k_norm<decltype(in)>, dim3((unsigned)partials, (unsigned)p.batch), room, p, at.partial); });
+  if (e != cudaSuccess) return e;
+  with_types(p.type, p.out_type, [&](auto in, auto out) {
+    e = launch_plain(k_start<decltype(in), decltype(out)>, dim3((unsigned)std::min<long long>(1024, cdiv(elements, 2048)), (unsigned)p.batch), room, p, at.partial, partials,
+                     p.steps > 0 ? at.x[0] : none, (float)scale);
+  });
+  const auto map = [&](CUtensorMap* t, const Image& im, int cols, int box_rows) {
+    return make_map(t, kF16, im.at, cols, im.rows, im.ld, 2LL * p.batch, (long long)im.rows * im.ld, box_rows);
+  };
+  for (int i = 0; i < p.steps && e == cudaSuccess; ++i) {
     const float* const c = p.coefficients + 3 * i;
-    k_batch_product<<<square, 256, 0, room.stream>>>(x, x, s, m, m, n, true, nullptr, 0.f, 0.f, 0.f);
-    k_batch_product<<<square, 256, 0, room.stream>>>(s, s, f, m, m, m, false, s, c[0], c[1], c[2]);
-    k_batch_product<<<wide, 256, 0, room.stream>>>(f, x, y, m, n, m, false, nullptr, 0.f, 0.f, 0.f);
-    std::swap(x, y);
+    const Growth g = grow(most, c[0], c[1], c[2]);
+    const double scale_s = scale_for(most * most), scale_p = scale_for(std::max(g.factor, 1e-3));
+    const double next = std::max(g.value, 1e-3), scale_next = scale_for(next);
+    const bool last = i + 1 == p.steps;
+    const Image &x = at.x[i & 1], &y = at.x[(i + 1) & 1];
+    const auto product = [&](auto tag, OrthogonalArgs& a) {
+      using J = typename decltype(tag)::Type;
+      a.error_flag = room.error_flag;
+      a.batch = p.batch;
+      const long long items = J::tiles(a.rows, a.cols) * p.batch;
+      if (items > INT_MAX) return cudaErrorInvalidValue;
+      return launch<J>(a, (unsigned)std::min<long long>(kSms, items), room);
+    };
+    OrthogonalArgs gram{}, poly{}, move{};
+    gram.rows = gram.cols = m;
+    gram.k = tall ? p.rows : p.cols;
+    gram.factor = (float)(scale_s / (scale * scale));
+    gram.to = at.s;
+    poly.rows = poly.cols = poly.k = m;
+    poly.factor = (float)(c[2] * scale_p / (scale_s * scale_s));
+    poly.diagonal = (float)(c[0] * scale_p);
+    poly.linear = (float)(c[1] * scale_p / scale_s);
+    poly.s = at.s;
+    poly.to = at.p;
+    move.rows = p.rows;
+    move.cols = p.cols;
+    move.k = m;
+    move.factor = (float)(last ? p.scale / (scale_p * scale) : scale_next / (scale_p * scale));
+    move.to = y;
+    if (last) {
+      move.out = p.out;
+      move.out_type = p.out_type;
+      move.ldo = p.ldo;
+      move.stride_o = p.stride_o;
+      move.vec_o = even(p.out, p.ldo, size_of(p.out_type)) && (p.batch == 1 || p.stride_o * size_of(p.out_type) % 16 == 0);
+    }
+    const auto step = [&](auto width) {
+      constexpr int BN = decltype(width)::value;
+      const bool maps = map(&poly.a, at.s, m, kBM) && map(&poly.b, at.s, m, BN) &&
+                        (tall ? map(&gram.a, x, p.cols, kBK) && map(&gram.b, x, p.cols, kBK) && map(&move.a, x, p.cols, kBM) && map(&move.b, at.p, m, BN)
+                              : map(&gram.a, x, p.cols, kBM) && map(&gram.b, x, p.cols, BN) && map(&move.a, at.p, m, kBM) && map(&move.b, x, p.cols, kBK));
+      if (!maps) return cudaErrorNotSupported;
+      cudaError_t q = tall ? product(Tag<OrthogonalJob<kGram, BN, true, true>>(), gram) : product(Tag<OrthogonalJob<kGram, BN, false, false>>(), gram);
+      if (q == cudaSuccess) q = product(Tag<OrthogonalJob<kPolynomial, BN, false, false>>(), poly);
+      if (q == cudaSuccess) q = tall ? product(Tag<OrthogonalJob<kMove, BN, false, false>>(), move) : product(Tag<OrthogonalJob<kMove, BN, false, true>>(), move);
+      return q;
+    };
+    // narrower tiles where the wider ones would leave SMs without any
+    const long long blocks = cdiv(m, 128);
+    e = p.batch * blocks * (blocks + 1) / 2 >= kSms ? step(std::integral_constant<int, 128>()) : step(std::integral_constant<int, 64>());
+    most = next;
+    scale = scale_next;
   }
-  const dim3 grid((unsigned)std::min<long long>(1024, cdiv((long long)m * n, 256)), 1, (unsigned)p.batch);
-  with_type(p.out_type, [&](auto out) { k_leave<decltype(out)><<<grid, 256, 0, room.stream>>>(p, x, m, n); });
-  *room.launches += 2 + 3 * p.steps;
-  return cudaGetLastError();
+  return e;
 }
 
 }  // namespace gcn_admm_grouped

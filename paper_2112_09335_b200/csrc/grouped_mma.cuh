@@ -29,7 +29,7 @@ namespace gcn_admm_grouped {
 
 using gtc::smem_u32;
 
-constexpr int kBM = 128, kBK = 64, kSegment = 4;   // rows of a tile; reduction steps of a chunk; chunks of a segment
+constexpr int kBM = 128, kBK = 64;   // rows of a tile; reduction steps of a chunk
 constexpr int kATile = kBM * kBK * 2;              // bytes of one part of an operand tile of A
 constexpr int kGroup64 = kBK * 128;                // bytes between groups of 64 in an MN-major tile
 constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps, kFirstProducer = kMmaWarp + 1;
@@ -220,7 +220,7 @@ struct Raw<unsigned short> {
 };
 
 // The shared loop.  A job J says what the items are, where operand tiles come from and what becomes of a tile's sums:
-//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kMeets (finish() has barriers of the epilogue warps)
+//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kSegment (chunks), kMeets (finish() has barriers of the epilogue warps)
 //   J(args, tables)                   built by every thread; setup(): tables in shared memory, by the whole block, between barriers
 //   bool item(unsigned i, Item&)      the i-th item, false behind the last; Item has chunks (of the reduction, maybe none), n (columns) and tail
 //                                     (steps of the last chunk that count, where rows behind them hold other data; else 64)
@@ -230,7 +230,7 @@ struct Raw<unsigned short> {
 template <class J>
 __global__ void __launch_bounds__(Geometry<J::kParts, J::kBN, J::kTma>::kThreads, 1) k_products(const __grid_constant__ typename J::Args args) {
   using G = Geometry<J::kParts, J::kBN, J::kTma>;
-  constexpr int S = G::kStages, BN = J::kBN, PARTS = J::kParts;
+  constexpr int S = G::kStages, BN = J::kBN, PARTS = J::kParts, kSegment = J::kSegment;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) Bars bars;
   __shared__ uint32_t tmem_slot;
