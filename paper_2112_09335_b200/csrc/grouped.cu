@@ -17,6 +17,8 @@ __device__ __forceinline__ void put(float* at, float x) { *at = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* at, float x) { *at = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void put(__half* at, float x) { *at = __float2half_rn(x); }
 
+constexpr int kSms = 148;
+
 // ---- groups of rows ----------------------------------------------------------------------------------
 // Rows of a group: offsets[g] .. offsets[g+1] cut to 0 .. rows, none where they descend.  Whatever the offsets hold, no row outside of
 // the matrices is touched.  Offsets are read as they are when the kernel runs.
@@ -24,6 +26,24 @@ __device__ __forceinline__ int2 group_rows(const int* offsets, int g, int rows) 
   const volatile int* const at = offsets + g;
   const int lo = min(max(at[0], 0), rows);
   return make_int2(lo, max(lo, min(at[1], rows)));
+}
+
+// v[g] = the sum of v up to g.  By one warp.
+template <typename V>
+__device__ __forceinline__ void scan(V* v, int count) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long before = 0;
+  for (int g0 = 0; g0 < count; g0 += 32) {
+    unsigned long long x = g0 + lane < count ? (unsigned long long)v[g0 + lane] : 0ull;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
+    }
+    x += before;
+    before = __shfl_sync(0xffffffffu, x, 31);
+    if (g0 + lane < count) v[g0 + lane] = sizeof(V) == 4 ? (V)min(x, (unsigned long long)INT_MAX) : (V)x;   // more tiles than that no memory has room for
+  }
 }
 
 // Which item belongs to which group: every block counts for itself (1024 groups are 4 loads a thread and a scan by one warp; a launch
@@ -34,22 +54,6 @@ struct Groups {
   int count;
   __device__ __forceinline__ Groups(uint8_t* tables, int count_)
       : ends(reinterpret_cast<unsigned*>(tables)), begin(reinterpret_cast<int*>(tables) + kMaxGroups), end(reinterpret_cast<int*>(tables) + 2 * kMaxGroups), count(count_) {}
-  // ends[g] = items of group g alone before, of all up to g afterwards, and the total.  By one warp.
-  __device__ __forceinline__ static void scan(unsigned* v, int count) {
-    const int lane = threadIdx.x & 31;
-    unsigned long long before = 0;
-    for (int g0 = 0; g0 < count; g0 += 32) {
-      unsigned long long x = g0 + lane < count ? v[g0 + lane] : 0u;
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const unsigned long long y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
-      }
-      x += before;
-      before = __shfl_sync(0xffffffffu, x, 31);
-      if (g0 + lane < count) v[g0 + lane] = (unsigned)min(x, (unsigned long long)INT_MAX);   // more than any memory has room for
-    }
-  }
   // The group of item i < ends[count - 1], from `g` on; `before`: items ahead of it.
   __device__ __forceinline__ int find(unsigned i, unsigned& before) const {
     int lo = 0, hi = count - 1;
@@ -62,29 +66,31 @@ struct Groups {
     return lo;
   }
 };
-constexpr int kTableBytes = 4 * kMaxGroups * 4 + 16;
+constexpr int kTableBytes = 4 * kMaxGroups * 4 + 16 + (kSms + 1) * 8;
 
 // ---- y = x W_g ---------------------------------------------------------------------------------------
 struct ProductArgs {
   CUtensorMap a, b;      // of x and of the weights, where tiles are copied by TMA
   Product p;
   int* error_flag;
-  bool vec_x, vec_w, vec_y;   // 16-byte boundaries
+  bool vec_x, vec_w, vec_y;   // rows start on 16-byte boundaries
 };
 
-template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA>
+template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA, bool PAIR = false, bool VEC = false>
 struct ProductJob {
   using T = T_;
   using Args = ProductArgs;
   static constexpr int kParts = PARTS, kBN = BN, kSegment = 4;
-  static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kMeets = false;
+  static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kMeets = false, kPair = PAIR;
+  static constexpr int kTileRows = PAIR ? 2 * kBM : kBM;
   struct Item {
     int chunks, n, tail, g, row0, left, col0;
   };
   const Args& a;
   Groups groups;
-  int tiles_n;
-  __device__ __forceinline__ ProductJob(const Args& args, uint8_t* tables) : a(args), groups(tables, args.p.groups), tiles_n((args.p.n + BN - 1) / BN) {}
+  int tiles_n, rank;
+  __device__ __forceinline__ ProductJob(const Args& args, uint8_t* tables, int rank_)
+      : a(args), groups(tables, args.p.groups), tiles_n((args.p.n + BN - 1) / BN), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return PARTS > 1 || a.p.type == kBf16; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {
@@ -92,17 +98,23 @@ struct ProductJob {
       const int2 r = group_rows(a.p.offsets, g, (int)a.p.rows);
       groups.begin[g] = r.x;
       groups.end[g] = r.y;
-      groups.ends[g] = (unsigned)min((unsigned long long)((r.y - r.x + kBM - 1) / kBM) * tiles_n, (unsigned long long)INT_MAX);
+      groups.ends[g] = (unsigned)min((unsigned long long)((r.y - r.x + kTileRows - 1) / kTileRows) * tiles_n, (unsigned long long)INT_MAX);
     }
     __syncthreads();
-    if (threadIdx.x < 32) Groups::scan(groups.ends, groups.count);
+    if (threadIdx.x < 32) scan(groups.ends, groups.count);
   }
-  __device__ __forceinline__ bool item(unsigned i, Item& it) const {
+  struct Walk {
+    unsigned i, step;
+  };
+  __device__ __forceinline__ Walk start(unsigned worker, unsigned workers) const { return Walk{worker, workers}; }
+  __device__ __forceinline__ bool next(Walk& at, Item& it) const {
+    const unsigned i = at.i;
     if (i >= groups.ends[groups.count - 1]) return false;
+    at.i += at.step;
     unsigned before;
     it.g = groups.find(i, before);
     const unsigned local = i - before, tile = local / tiles_n;
-    it.row0 = groups.begin[it.g] + (int)tile * kBM;
+    it.row0 = groups.begin[it.g] + (int)tile * kTileRows + rank * kBM;
     it.left = groups.end[it.g] - it.row0;
     it.col0 = (int)(local - tile * tiles_n) * BN;
     it.n = a.p.n - it.col0;
@@ -110,35 +122,31 @@ struct ProductJob {
     it.tail = kBK;
     return true;
   }
+  template <bool THERE>
   __device__ __forceinline__ void copy(const Item& it, int c, uint32_t tile, uint32_t bar) const {
-    const int boxes = TRANSPOSED ? BN / 64 : min(BN / 64, (it.n + 63) / 64);   // columns behind the last are left out: they meet no result
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)(kATile + boxes * kGroup64)) : "memory");
-    copy_2d(tile, &a.a, c * kBK, it.row0, bar);
+    constexpr int kBCols = PAIR ? BN / 2 : BN;
+    const int col0 = it.col0 + rank * kBCols;
+    const int boxes = TRANSPOSED ? kBCols / 64 : min(kBCols / 64, max(0, (a.p.n - col0 + 63) / 64));   // columns behind the last are left out: they meet no result
+    expect<THERE>(bar, (uint32_t)(kATile + boxes * kGroup64));
+    copy_2d<THERE>(tile, &a.a, c * kBK, it.row0, bar);
     if constexpr (TRANSPOSED) {
-      copy_3d(tile + kATile, &a.b, c * kBK, it.col0, it.g, bar);
+      copy_3d<THERE>(tile + kATile, &a.b, c * kBK, col0, it.g, bar);
     } else {
-      for (int b = 0; b < boxes; ++b) copy_3d(tile + kATile + b * kGroup64, &a.b, it.col0 + 64 * b, c * kBK, it.g, bar);
+      for (int b = 0; b < boxes; ++b) copy_3d<THERE>(tile + kATile + b * kGroup64, &a.b, col0 + 64 * b, c * kBK, it.g, bar);
     }
   }
-  template <int NA, int NB>
-  __device__ __forceinline__ void load(const Item& it, int c, int t, Raw<T> (&ra)[NA], Raw<T> (&rb)[NB]) const {
-    const T* const x = static_cast<const T*>(a.p.x) + (long long)it.row0 * a.p.ldx;
+  __device__ __forceinline__ void load_a(const Item& it, int c, int at, Raw<T>& raw) const {
+    const int row = at >> 3, k = c * kBK + (at & 7) * 8;
+    raw.template load<VEC>(static_cast<const T*>(a.p.x) + (long long)(it.row0 + row) * a.p.ldx + k, row < it.left ? a.p.k - k : 0);
+  }
+  __device__ __forceinline__ void load_b(const Item& it, int c, int at, Raw<T>& raw) const {
     const T* const w = static_cast<const T*>(a.p.w) + (long long)it.g * a.p.stride_w;
-#pragma unroll
-    for (int u = 0; u < NA; ++u) {
-      const int at = t + 256 * u, row = at >> 3, k = c * kBK + (at & 7) * 8;
-      ra[u].load(x + row * a.p.ldx + k, row < it.left ? a.p.k - k : 0, a.vec_x);
-    }
-#pragma unroll
-    for (int u = 0; u < NB; ++u) {
-      const int at = t + 256 * u;
-      if constexpr (TRANSPOSED) {
-        const int col = at >> 3, k = c * kBK + (at & 7) * 8;
-        rb[u].load(w + (it.col0 + col) * a.p.ldw + k, col < it.n ? a.p.k - k : 0, a.vec_w);
-      } else {
-        const int k = c * kBK + at / (BN / 8), col = at % (BN / 8) * 8;
-        rb[u].load(w + k * a.p.ldw + it.col0 + col, k < a.p.k ? it.n - col : 0, a.vec_w);
-      }
+    if constexpr (TRANSPOSED) {
+      const int col = at >> 3, k = c * kBK + (at & 7) * 8;
+      raw.template load<VEC>(w + (long long)(it.col0 + col) * a.p.ldw + k, col < it.n ? a.p.k - k : 0);
+    } else {
+      const int k = c * kBK + at / (BN / 8), col = at % (BN / 8) * 8;
+      raw.template load<VEC>(w + (long long)k * a.p.ldw + it.col0 + col, k < a.p.k ? it.n - col : 0);
     }
   }
   template <int NC>
@@ -151,140 +159,222 @@ struct ProductJob {
 };
 
 // ---- dw_g = x_g^T y_g --------------------------------------------------------------------------------
-// A group's rows are cut into pieces of at most `piece` chunks where it has more, so that few tiles still fill the chip and no long group is
-// walked by one block while the others wait.  The pieces' sums go to the workspace, and the block that finishes a tile's last piece adds
-// them up, always in the order of the pieces.
+// Tiles of groups of unequal length do not share out evenly.  Workers (blocks, or pairs of blocks) take whole tiles in turn while
+// there is more than one round of them left (all of them, from kWholeRounds on), so that those at work at the same time read the same group's rows; what remains, up to two rounds, is seen as one
+// stretch of chunks (group, tile, chunk of rows in this order), of which every worker gets what brings it to the mean.  So few
+// tiles still fill the chip, and no long group is walked by one worker while the others wait.  (169343 x 256 x 40 in 32 groups, 64 tiles: 143 us in
+// pieces of a length fixed beforehand, 88 us so; all work as one stretch took 259 us for 16384 x 2048 x 1024 in 16 groups, where each worker read rows of its
+// own, instead of 118.)
+// A tile that several workers share is put together from their sums, which they leave in the workspace: whoever comes last of up
+// to kJoin workers adds theirs up, in the order of the work; where there are more, whoever comes last of these adds those up in turn.
 struct ProductTnArgs {
   CUtensorMap a, b;
   ProductTn p;
   int* error_flag;
-  bool vec_x, vec_y, vec_w;
-  int piece;            // chunks
-  unsigned slots;       // tiles of sums the workspace has room for
-  float* space;
-  unsigned* tickets;
+  bool vec_x, vec_y, vec_w;   // rows start on 16-byte boundaries
+  float* space;         // two tiles of sums for every block
+  unsigned* tickets;    // three for every block
 };
+constexpr int kJoin = 12;        // one block reads the sums of all, one after the other: 148 of them took 148 us
+constexpr int kWholeRounds = 4;  // of whole tiles, from which no stretch is made: its sums, at the end of all work, cost as much as the last round's gaps
+constexpr int kLeastChunks = 4;  // of a worker: below, the sums cost more than what they spread
 
-template <typename T_, int PARTS, int BN, bool TMA>
+template <typename T_, int PARTS, int BN, bool TMA, bool PAIR = false, bool VEC = false>
 struct ProductTnJob {
   using T = T_;
   using Args = ProductTnArgs;
+  using Size = unsigned long long;
   static constexpr int kParts = PARTS, kBN = BN, kSegment = 4;
-  static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kMeets = true;
+  static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kMeets = true, kPair = PAIR;
+  static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kRanks = PAIR ? 2 : 1;
   struct Item {
     int chunks, n, tail, g, row0, end, m0, col0;
-    int pieces;
-    unsigned piece, tile;
+    unsigned from, pieces, piece;   // first worker of the tile, number of them, which of them this one is
+  };
+  struct Walk {
+    Size at, end;      // of the stretch
+    unsigned round, worker;
   };
   const Args& a;
-  Groups groups;
-  unsigned* slots;   // [groups] first of the group's tiles of sums
+  Size* ends;          // [groups] chunks of this group and all before it
+  int *begin, *end;    // [groups] rows
   int* last;
-  int tiles_n, tiles, longest;   // longest: chunks of a piece
-  __device__ __forceinline__ ProductTnJob(const Args& args, uint8_t* tables)
-      : a(args), groups(tables, args.p.groups), slots(reinterpret_cast<unsigned*>(tables) + 3 * kMaxGroups), last(reinterpret_cast<int*>(tables) + 4 * kMaxGroups),
-        tiles_n((args.p.nb + BN - 1) / BN), tiles(tiles_n * ((args.p.ka + kBM - 1) / kBM)), longest(args.piece) {}
+  Size* shares;        // [workers + 1] where each worker's part of the stretch begins
+  int count, tiles_n, tiles, rank;
+  unsigned workers, rounds;
+  __device__ __forceinline__ ProductTnJob(const Args& args, uint8_t* tables, int rank_)
+      : a(args), ends(reinterpret_cast<Size*>(tables)), begin(reinterpret_cast<int*>(tables) + 2 * kMaxGroups), end(reinterpret_cast<int*>(tables) + 3 * kMaxGroups),
+        last(reinterpret_cast<int*>(tables) + 4 * kMaxGroups), shares(reinterpret_cast<Size*>(tables) + 2 * kMaxGroups + 2), count(args.p.groups), tiles_n((args.p.nb + BN - 1) / BN),
+        tiles(tiles_n * ((args.p.ka + kTileRows - 1) / kTileRows)), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return PARTS > 1 || a.p.type == kBf16; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
-  __device__ __forceinline__ static int pieces_of(int rows, int piece, int& per) {
-    const int chunks = (rows + kBK - 1) / kBK, want = chunks > piece ? (chunks + piece - 1) / piece : 1;
-    per = want > 1 ? (chunks + want - 1) / want : chunks;
-    return want > 1 ? (chunks + per - 1) / per : 1;
-  }
+  // Chunks of a tile of group g; a group without rows has one, which writes zeros.
+  __device__ __forceinline__ unsigned chunks_of(int g) const { return (unsigned)max(1, (end[g] - begin[g] + kBK - 1) / kBK); }
   __device__ __forceinline__ void setup() {
-    count_items();
-    __syncthreads();
-    if (slots[groups.count - 1] > a.slots) {   // groups that overlap: nothing is cut then
-      longest = INT_MAX;
-      __syncthreads();
-      count_items();
-    }
-  }
-  __device__ __forceinline__ void count_items() {
-    for (int g = threadIdx.x; g < groups.count; g += blockDim.x) {
+    for (int g = threadIdx.x; g < count; g += blockDim.x) {
       const int2 r = group_rows(a.p.offsets, g, (int)a.p.rows);
-      int per;
-      const unsigned long long items = (unsigned long long)pieces_of(r.y - r.x, longest, per) * tiles;
-      groups.begin[g] = r.x;
-      groups.end[g] = r.y;
-      groups.ends[g] = (unsigned)min(items, (unsigned long long)INT_MAX);
-      slots[g] = items > (unsigned)tiles ? groups.ends[g] : 0u;
+      begin[g] = r.x;
+      end[g] = r.y;
+      ends[g] = (Size)chunks_of(g) * tiles;
     }
     __syncthreads();
-    if (threadIdx.x < 32) Groups::scan(groups.ends, groups.count);
-    else if (threadIdx.x < 64) Groups::scan(slots, groups.count);
+    if (threadIdx.x < 32) scan(ends, count);
+    __syncthreads();
+    const Size total = ends[count - 1], all = (Size)count * tiles;
+    workers = (unsigned)min((Size)gridDim.x / kRanks, max((Size)1, total / kLeastChunks));
+    rounds = (unsigned)(all / workers >= kWholeRounds ? (all + workers - 1) / workers : all / workers >= 2 ? all / workers - 1 : 0);
+    if (all / workers >= kWholeRounds) return;
+    // what a worker is short of the mean after its rounds, and of the stretch as much in proportion (and one chunk, so that none is left out)
+    if (threadIdx.x < workers) {
+      Size load = 0;
+      for (unsigned r = 0; r < rounds; ++r) load += chunks_of((int)(((Size)r * workers + threadIdx.x) / tiles));
+      shares[threadIdx.x] = total / workers > load ? total / workers - load : 1;
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      scan(shares, (int)workers);
+      __syncwarp();
+      const Size stretch = total - first_of_stretch(), sum = shares[workers - 1];
+      for (int p = (int)((workers - 1) / 32 * 32); p >= 0; p -= 32) {   // from behind: share p goes to place p + 1
+        const unsigned w = (unsigned)p + threadIdx.x;
+        const Size to = w < workers ? w + 1 + (Size)((double)(stretch - workers) * ((double)shares[w] / (double)sum)) : 0;
+        __syncwarp();
+        if (w < workers) shares[w + 1] = w + 1 == workers ? stretch : to;
+        __syncwarp();
+      }
+      if (threadIdx.x == 0) shares[0] = 0;
+    }
   }
-  __device__ __forceinline__ bool item(unsigned i, Item& it) const {
-    if (i >= groups.ends[groups.count - 1]) return false;
-    unsigned before;
-    it.g = groups.find(i, before);
-    const unsigned local = i - before;
-    const int begin = groups.begin[it.g], end = groups.end[it.g];
-    int per;
-    it.pieces = pieces_of(end - begin, longest, per);
-    it.piece = local / tiles;
-    it.tile = local - it.piece * tiles;
-    it.m0 = (int)(it.tile / tiles_n) * kBM;
-    it.col0 = (int)(it.tile % tiles_n) * BN;
+  // Chunks ahead of the stretch, which begins with a whole tile.
+  __device__ __forceinline__ Size first_of_stretch() const {
+    const Size tile = (Size)rounds * workers;
+    const int g = (int)(tile / tiles);
+    return (g > 0 ? ends[g - 1] : 0) + (tile - (Size)g * tiles) * chunks_of(g);
+  }
+  __device__ __forceinline__ unsigned owner(Size at) const {
+    unsigned lo = 0, hi = workers - 1;
+    while (lo < hi) {
+      const unsigned mid = (lo + hi) >> 1;
+      if (shares[mid + 1] > at) hi = mid;
+      else lo = mid + 1;
+    }
+    return lo;
+  }
+  __device__ __forceinline__ Walk start(unsigned worker, unsigned) const {
+    if (worker >= workers) return Walk{0, 0, rounds, worker};
+    if ((Size)rounds * workers >= (Size)count * tiles) return Walk{0, 0, 0, worker};   // no stretch
+    return Walk{shares[worker], shares[worker + 1], 0, worker};
+  }
+  __device__ __forceinline__ bool next(Walk& w, Item& it) const {
+    it.pieces = 1;
+    it.piece = 0;
+    it.from = w.worker;
+    unsigned tile, c0 = 0, per, c1;
+    if (w.round < rounds) {
+      const Size i = (Size)w.round * workers + w.worker;
+      if (i >= (Size)count * tiles) return false;
+      ++w.round;
+      it.g = (int)(i / tiles);
+      tile = (unsigned)(i - (Size)it.g * tiles);
+      c1 = per = chunks_of(it.g);
+    } else {
+      if (w.at >= w.end) return false;
+      const Size ahead = first_of_stretch(), at = ahead + w.at;
+      int lo = 0, hi = count - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ends[mid] > at) hi = mid;
+        else lo = mid + 1;
+      }
+      it.g = lo;
+      per = chunks_of(lo);
+      const Size local = at - (lo > 0 ? ends[lo - 1] : 0);
+      tile = (unsigned)(local / per);
+      c0 = (unsigned)(local - (Size)tile * per);
+      c1 = (unsigned)min((Size)per, c0 + (w.end - w.at));
+      if (c0 > 0 || c1 < per) {
+        const Size begins = w.at - c0;
+        it.from = owner(begins);
+        it.pieces = owner(begins + per - 1) - it.from + 1;
+        it.piece = w.worker - it.from;
+      }
+      w.at += c1 - c0;
+    }
+    it.m0 = (int)(tile / tiles_n) * kTileRows + rank * kBM;
+    it.col0 = (int)(tile % tiles_n) * BN;
     it.n = a.p.nb - it.col0;
-    it.row0 = begin + (int)it.piece * per * kBK;
-    it.end = (int)it.piece + 1 < it.pieces ? it.row0 + per * kBK : end;
+    it.row0 = begin[it.g] + (int)c0 * kBK;
+    it.end = c1 < per ? begin[it.g] + (int)c1 * kBK : end[it.g];
     it.chunks = (it.end - it.row0 + kBK - 1) / kBK;
     it.tail = it.end - it.row0 - (it.chunks - 1) * kBK;
     return true;
   }
+  template <bool THERE>
   __device__ __forceinline__ void copy(const Item& it, int c, uint32_t tile, uint32_t bar) const {
-    const int boxes_a = min(kBM / 64, (a.p.ka - it.m0 + 63) / 64), boxes_b = min(BN / 64, (it.n + 63) / 64), row = it.row0 + c * kBK;
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)((boxes_a + boxes_b) * kGroup64)) : "memory");
-    for (int b = 0; b < boxes_a; ++b) copy_2d(tile + b * kGroup64, &a.a, it.m0 + 64 * b, row, bar);
-    for (int b = 0; b < boxes_b; ++b) copy_2d(tile + kATile + b * kGroup64, &a.b, it.col0 + 64 * b, row, bar);
+    constexpr int kBCols = PAIR ? BN / 2 : BN;
+    const int col0 = it.col0 + rank * kBCols, row = it.row0 + c * kBK;
+    const int boxes_a = min(kBM / 64, max(0, (a.p.ka - it.m0 + 63) / 64)), boxes_b = min(kBCols / 64, max(0, (a.p.nb - col0 + 63) / 64));
+    expect<THERE>(bar, (uint32_t)((boxes_a + boxes_b) * kGroup64));
+    for (int b = 0; b < boxes_a; ++b) copy_2d<THERE>(tile + b * kGroup64, &a.a, it.m0 + 64 * b, row, bar);
+    for (int b = 0; b < boxes_b; ++b) copy_2d<THERE>(tile + kATile + b * kGroup64, &a.b, col0 + 64 * b, row, bar);
   }
-  template <int NA, int NB>
-  __device__ __forceinline__ void load(const Item& it, int c, int t, Raw<T> (&ra)[NA], Raw<T> (&rb)[NB]) const {
-    const T* const x = static_cast<const T*>(a.p.x) + it.m0;
-    const T* const y = static_cast<const T*>(a.p.y) + it.col0;
+  __device__ __forceinline__ void load_a(const Item& it, int c, int at, Raw<T>& raw) const {
+    const int col = it.m0 + at % (kBM / 8) * 8, row = it.row0 + c * kBK + at / (kBM / 8);
+    raw.template load<VEC>(static_cast<const T*>(a.p.x) + (long long)row * a.p.ldx + col, row < it.end ? a.p.ka - col : 0);
+  }
+  __device__ __forceinline__ void load_b(const Item& it, int c, int at, Raw<T>& raw) const {
+    const int col = it.col0 + at % (BN / 8) * 8, row = it.row0 + c * kBK + at / (BN / 8);
+    raw.template load<VEC>(static_cast<const T*>(a.p.y) + (long long)row * a.p.ldy + col, row < it.end ? a.p.nb - col : 0);
+  }
+  // The sums of a worker: of the tile it begins (but does not end) or of the one it continues.  It has at most one of each.
+  template <int NC>
+  __device__ __forceinline__ float* sums(unsigned worker, bool begins, int warp) const {
+    return a.space + (((size_t)worker * 2 + begins) * kRanks + rank) * (kBM * BN) + (size_t)warp * NC * 32 + (threadIdx.x & 31);
+  }
+  // Leaves acc with the others' and says, to all epilogue warps, whether all `of` are there.
+  template <int NC>
+  __device__ __forceinline__ bool leave(const float (&acc)[NC], float* at, unsigned* ticket, unsigned of, int columns) const {
 #pragma unroll
-    for (int u = 0; u < NA; ++u) {
-      const int at = t + 256 * u, col = at % (kBM / 8) * 8;
-      const long long row = it.row0 + c * kBK + at / (kBM / 8);
-      ra[u].load(x + row * a.p.ldx + col, row < it.end ? a.p.ka - it.m0 - col : 0, a.vec_x);
+    for (int c = 0; c < NC; ++c)
+      if (c < columns) __stcg(at + c * 32, acc[c]);
+    __threadfence();
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (threadIdx.x == 0) {
+      *last = atomicAdd(ticket, 1u) + 1 == of;
+      if (*last) *ticket = 0u;
+      __threadfence();
     }
-#pragma unroll
-    for (int u = 0; u < NB; ++u) {
-      const int at = t + 256 * u, col = at % (BN / 8) * 8;
-      const long long row = it.row0 + c * kBK + at / (BN / 8);
-      rb[u].load(y + row * a.p.ldy + col, row < it.end ? it.n - col : 0, a.vec_y);
-    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const bool all = *last != 0;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    return all;
   }
   template <int NC>
   __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], uint8_t* buf, int warp) const {
-    const int lane = threadIdx.x & 31;
-    if (it.pieces > 1) {
-      const unsigned first = it.g > 0 ? slots[it.g - 1] : 0u;   // (scanned)
-      float* const sums = a.space + (size_t)(first + it.tile) * (kBM * BN) + (size_t)warp * NC * 32 + lane;
-      const size_t step = (size_t)tiles * (kBM * BN);
-      float* const mine = sums + it.piece * step;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) __stcg(mine + c * 32, acc[c]);
-      __threadfence();
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (threadIdx.x == 0) {
-        unsigned* const ticket = a.tickets + first + it.tile;
-        const unsigned done = atomicAdd(ticket, 1u);
-        *last = done + 1 == (unsigned)it.pieces;
-        if (*last) *ticket = 0u;
-        __threadfence();
-      }
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (!*last) return;
-      __threadfence();
-#pragma unroll
-      for (int c = 0; c < NC; ++c) acc[c] = 0.f;
-      for (int s = 0; s < it.pieces; ++s)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) acc[c] += __ldcg(sums + s * step + c * 32);
-    }
     const int row = it.m0 + (warp & 3) * 32, col = it.col0 + (warp >> 2) * NC;
+    if (it.pieces > 1) {
+      const int columns = a.p.ka - row > 0 ? a.p.nb - col : 0;   // that come to anything
+      const auto of_piece = [&](unsigned piece) { return sums<NC>(it.from + piece, piece == 0, warp); };
+      const auto add_up = [&](unsigned from, unsigned to, unsigned step) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[c] = 0.f;
+        for (unsigned q = from; q < to; q += step) {
+          const float* const at = of_piece(q);
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            if (c < columns) acc[c] += __ldcg(at + c * 32);
+        }
+      };
+      const unsigned join = it.piece / kJoin, first = join * kJoin, behind = min(it.pieces, first + kJoin);
+      // tickets of the blocks that begin a tile, that begin a later join of one, and of the joins of a tile
+      const unsigned all = gridDim.x, mine = (it.from + first) * kRanks + rank;
+      if (!leave<NC>(acc, of_piece(it.piece), a.tickets + (join > 0 ? all : 0u) + mine, behind - first, columns)) return;
+      add_up(first, behind, 1);
+      if (it.pieces > kJoin) {
+        if (!leave<NC>(acc, of_piece(first), a.tickets + 2 * all + it.from * kRanks + rank, (it.pieces + kJoin - 1) / kJoin, columns)) return;
+        add_up(0, it.pieces, kJoin);
+      }
+    }
     const long long at = it.g * a.p.stride_dw + row * a.p.lddw + col;
     void* const dw = a.p.out_type == kF32 ? (void*)(static_cast<float*>(a.p.dw) + at) : (void*)(static_cast<unsigned short*>(a.p.dw) + at);
     store_rows<NC>(acc, buf, dw, a.p.lddw, a.p.out_type, a.vec_w, a.p.ka - row, a.p.nb - col);
@@ -424,12 +514,12 @@ template <Stage STAGE, int BN, bool A_MN, bool B_MN>
 struct OrthogonalJob {
   using Args = OrthogonalArgs;
   static constexpr int kParts = 2, kBN = BN, kSegment = 1;
-  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kSymmetric = STAGE != kMove;
+  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kPair = false, kSymmetric = STAGE != kMove;
   struct Item {
     int chunks, n, tail, matrix, row0, col0;
   };
   const Args& a;
-  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*) : a(args) {}
+  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int) : a(args) {}
   __device__ __forceinline__ bool bf16() const { return false; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {}
@@ -438,10 +528,15 @@ struct OrthogonalJob {
     const long long m = (rows + kBM - 1) / kBM;
     return kSymmetric ? kBM / BN * (m * (m + 1) / 2) : m * ((cols + BN - 1) / BN);
   }
-  __device__ __forceinline__ bool item(unsigned i, Item& it) const {
-    const unsigned per = (unsigned)tiles(a.rows, a.cols);
+  struct Walk {
+    unsigned i, step;
+  };
+  __device__ __forceinline__ Walk start(unsigned worker, unsigned workers) const { return Walk{worker, workers}; }
+  __device__ __forceinline__ bool next(Walk& at, Item& it) const {
+    const unsigned per = (unsigned)tiles(a.rows, a.cols), i = at.i;
     it.matrix = (int)(i / per);
     if (it.matrix >= a.batch) return false;
+    at.i += at.step;
     const unsigned t = i - (unsigned)it.matrix * per;
     unsigned row, col;
     if constexpr (kSymmetric) {
@@ -462,23 +557,24 @@ struct OrthogonalJob {
     it.tail = kBK;
     return true;
   }
+  template <bool THERE>
   __device__ __forceinline__ void copy(const Item& it, int c, uint32_t tile, uint32_t bar) const {
     constexpr int kBTile = BN * kBK * 2;
     const int boxes_a = A_MN ? min(kBM / 64, (a.rows - it.row0 + 63) / 64) : kBM / 64, boxes_b = B_MN ? min(BN / 64, (it.n + 63) / 64) : BN / 64;
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)(2 * (boxes_a + boxes_b) * kGroup64)) : "memory");
+    expect<THERE>(bar, (uint32_t)(2 * (boxes_a + boxes_b) * kGroup64));
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
       const int z = part * a.batch + it.matrix;
       const uint32_t ta = tile + part * kATile, tb = tile + 2 * kATile + part * kBTile;
       if constexpr (A_MN) {
-        for (int b = 0; b < boxes_a; ++b) copy_3d(ta + b * kGroup64, &a.a, it.row0 + 64 * b, c * kBK, z, bar);
+        for (int b = 0; b < boxes_a; ++b) copy_3d<THERE>(ta + b * kGroup64, &a.a, it.row0 + 64 * b, c * kBK, z, bar);
       } else {
-        copy_3d(ta, &a.a, c * kBK, it.row0, z, bar);
+        copy_3d<THERE>(ta, &a.a, c * kBK, it.row0, z, bar);
       }
       if constexpr (B_MN) {
-        for (int b = 0; b < boxes_b; ++b) copy_3d(tb + b * kGroup64, &a.b, it.col0 + 64 * b, c * kBK, z, bar);
+        for (int b = 0; b < boxes_b; ++b) copy_3d<THERE>(tb + b * kGroup64, &a.b, it.col0 + 64 * b, c * kBK, z, bar);
       } else {
-        copy_3d(tb, &a.b, c * kBK, it.col0, z, bar);
+        copy_3d<THERE>(tb, &a.b, c * kBK, it.col0, z, bar);
       }
     }
   }
@@ -542,7 +638,8 @@ void with_types(int type, int out_type, const F& f) {
   });
 }
 
-constexpr int kSms = 148;
+// Whether tiles of 256 columns are well filled: pairs have no narrower ones.
+bool fits_pairs(int n) { return cdiv(n, 256) * 256 * 4 <= 5LL * n; }
 
 // Whether every row of a matrix starts on a 16-byte boundary.
 bool even(const void* p, long long ld, int size) { return reinterpret_cast<std::uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0; }
@@ -562,9 +659,9 @@ bool make_map(CUtensorMap* map, int type, const void* p, long long cols, long lo
 // A kernel that waits for its predecessor on the stream itself (gtc::enter_kernel), so that its launch runs beside that one's end.
 template <class J>
 cudaError_t launch(const typename J::Args& args, unsigned grid, const Room& room) {
-  using G = Geometry<J::kParts, J::kBN, J::kTma>;
+  using G = GeometryOf<J>;
   constexpr size_t smem = 1024 + G::kTablesAt + kTableBytes;
-  static_assert(smem + 1024 <= 232448, "shared memory of an SM");
+  static_assert(smem + 512 <= 232448, "shared memory of an SM");
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
@@ -579,11 +676,14 @@ cudaError_t launch(const typename J::Args& args, unsigned grid, const Room& room
   cfg.blockDim = dim3(G::kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = room.stream;
-  cudaLaunchAttribute behind{};
-  behind.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  behind.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &behind;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute with[2]{};
+  with[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  with[0].val.programmaticStreamSerializationAllowed = 1;
+  with[1].id = cudaLaunchAttributeClusterDimension;
+  with[1].val.clusterDim.x = 2;
+  with[1].val.clusterDim.y = with[1].val.clusterDim.z = 1;
+  cfg.attrs = with;
+  cfg.numAttrs = J::kPair ? 2 : 1;
   ++*room.launches;
   return cudaLaunchKernelEx(&cfg, k_products<J>, args);
 }
@@ -610,27 +710,26 @@ struct Tag {
 
 }  // namespace
 
-// Pieces of a weight gradient: the longest whose items give every SM one of about equal length.
+// Tiles of a weight gradient: 256 x 256 by pairs of blocks where both widths fill them, else 128 rows by what the columns need.
 struct TnPlan {
-  int bn, piece;
-  long long slots;
+  int bn, ranks;     // ranks: blocks of a tile
+  unsigned grid;
 };
 TnPlan plan(const ProductTn& p) {
   const bool wide = p.type != kF32;
-  TnPlan t;
-  t.bn = p.nb <= 64 ? 64 : p.nb <= 128 || !wide ? 128 : 256;
-  const long long tiles = cdiv(p.ka, kBM) * cdiv(p.nb, t.bn), chunks = cdiv(p.rows, kBK);
-  t.piece = (int)std::max<long long>(8, cdiv(chunks * tiles, kSms));
-  // A group of c > piece >= 8 chunks has at most 2 c / piece pieces, and such groups together at most 9/8 of the chunks of all rows.
-  t.slots = std::min<long long>(cdiv(9 * chunks, 4 * t.piece) * tiles, INT_MAX);
-  if (chunks <= t.piece) t.slots = 0;
+  const int size = size_of(p.type);
+  const bool pair = wide && p.rows > 0 && fits_pairs(p.ka) && fits_pairs(p.nb) && even(p.x, p.ldx, size) && even(p.y, p.ldy, size) && gcn_admm_host::encode_tiled() != nullptr;
+  TnPlan t{p.nb <= 64 ? 64 : p.nb <= 128 || !wide ? 128 : 256, pair ? 2 : 1, kSms};
+  // no more than there is work for: chunks at most, wherever the groups begin, and not fewer than tiles
+  const long long tiles = cdiv(p.ka, t.ranks * kBM) * cdiv(p.nb, t.bn), chunks = tiles * (cdiv(p.rows, kBK) + p.groups);
+  t.grid = (unsigned)std::min<long long>(kSms, t.ranks * std::max<long long>(1, chunks / kLeastChunks));
   return t;
 }
 std::size_t space_bytes(const ProductTn& p) {
   const TnPlan t = plan(p);
-  return (std::size_t)t.slots * kBM * t.bn * sizeof(float);
+  return 2ull * t.grid * kBM * t.bn * sizeof(float);
 }
-std::size_t tickets_of(const ProductTn& p) { return (std::size_t)plan(p).slots; }
+std::size_t tickets_of(const ProductTn& p) { return 3ull * plan(p).grid; }
 
 // The images of a call in its workspace.
 struct OrthogonalSpace {
@@ -670,6 +769,12 @@ cudaError_t enqueue(const Product& p, const Room& room) {
   a.vec_w = even(p.w, p.ldw, size) && (p.groups == 1 || p.stride_w * size % 16 == 0);
   a.vec_y = even(p.y, p.ldy, size_of(p.out_type));
   const long long tiles_m = std::min<long long>(p.rows, cdiv(p.rows, kBM) + p.groups);   // at most, wherever the groups begin
+  if (p.type != kF32 && a.vec_x && a.vec_w && fits_pairs(p.n) && std::min<long long>(p.rows, cdiv(p.rows, 2 * kBM) + p.groups) * cdiv(p.n, 256) >= kSms / 2) {
+    const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
+    if (make_map(&a.a, p.type, p.x, p.k, p.rows, p.ldx, 1, 0, kBM) && make_map(&a.b, p.type, p.w, w_cols, w_rows, p.ldw, p.groups, p.stride_w, p.transposed ? 128 : kBK))
+      return p.transposed ? launch<ProductJob<unsigned short, 1, 256, true, true, true>>(a, kSms, room) : launch<ProductJob<unsigned short, 1, 256, false, true, true>>(a, kSms, room);
+  }
+  const bool quads = a.vec_x && a.vec_w && p.k % 4 == 0 && (p.transposed || p.n % 4 == 0);   // rows of both operands are whole quads
   const auto pick = [&](auto tma) {
     // The widest tile that still gives every SM one
     const auto enough = [&](int bn) { return p.n > bn / 2 && tiles_m * cdiv(p.n, bn) >= kSms; };
@@ -686,6 +791,7 @@ cudaError_t enqueue(const Product& p, const Room& room) {
       constexpr bool T = decltype(turned)::value;
       if constexpr (decltype(tma)::value) return launch<ProductJob<unsigned short, 1, BN, T, true>>(a, grid, room);
       else if constexpr (BN == 256) return cudaErrorNotSupported;
+      else if (p.type == kF32 && quads) return launch<ProductJob<float, 3, BN, T, false, false, true>>(a, grid, room);
       else if (p.type == kF32) return launch<ProductJob<float, 3, BN, T, false>>(a, grid, room);
       else return launch<ProductJob<unsigned short, 1, BN, T, false>>(a, grid, room);
     };
@@ -708,18 +814,20 @@ cudaError_t enqueue(const ProductTn& p, const Room& room) {
   a.vec_y = even(p.y, p.ldy, size);
   a.vec_w = even(p.dw, p.lddw, size_of(p.out_type)) && (p.groups == 1 || p.stride_dw * size_of(p.out_type) % 16 == 0);
   const TnPlan t = plan(p);
-  a.piece = t.piece;
-  a.slots = (unsigned)t.slots;
   a.space = static_cast<float*>(room.space);
   a.tickets = room.tickets;
-  const long long items = cdiv(p.ka, kBM) * cdiv(p.nb, t.bn) * p.groups + t.slots;
-  const unsigned grid = (unsigned)std::min<long long>(kSms, items);
+  if (t.ranks == 2) {
+    if (!make_map(&a.a, p.type, p.x, p.ka, p.rows, p.ldx, 1, 0, kBK) || !make_map(&a.b, p.type, p.y, p.nb, p.rows, p.ldy, 1, 0, kBK)) return cudaErrorNotSupported;
+    return launch<ProductTnJob<unsigned short, 1, 256, true, true>>(a, t.grid, room);
+  }
+  const unsigned grid = t.grid;
   const auto width = [&](const auto& f) {
     return t.bn == 256 ? f(std::integral_constant<int, 256>()) : t.bn == 128 ? f(std::integral_constant<int, 128>()) : f(std::integral_constant<int, 64>());
   };
   if (p.type == kF32)
     return width([&](auto w) {
       if constexpr (decltype(w)::value == 256) return cudaErrorNotSupported;
+      else if (a.vec_x && a.vec_y && p.ka % 4 == 0 && p.nb % 4 == 0) return launch<ProductTnJob<float, 3, decltype(w)::value, false, false, true>>(a, grid, room);
       else return launch<ProductTnJob<float, 3, decltype(w)::value, false>>(a, grid, room);
     });
   if (p.rows > 0 && a.vec_x && a.vec_y && make_map(&a.a, p.type, p.x, p.ka, p.rows, p.ldx, 1, 0, kBK) && make_map(&a.b, p.type, p.y, p.nb, p.rows, p.ldy, 1, 0, kBK))

@@ -3,10 +3,15 @@
 // A block owns one SM and walks over work items, each a tile of 128 rows x kBN columns of some D = A B with a reduction of any length.
 //   warps 0-7    epilogue: tensor memory -> registers -> sums of segments -> result
 //   warp 8       matrix instructions (one lane issues)
-//   warp 9       copies of operand tiles by TMA, or warps 9-16: operand tiles through registers
+//   warp 9       copies of operand tiles by TMA (warp 10: clears what they bring from behind the end of a group), or warps 8-15: operand tiles through registers (warp 8 issues behind its part of a chunk; as a 17th
+//                warp the issuer left 96 registers a thread, too few for a chunk in flight)
 // Operand tiles are 64 steps of the reduction wide and lie in shared memory with the 128-byte swizzle, K-major (a row of the tile is
 // 128 bytes of the reduction) or MN-major (a row is one step of the reduction, 128 bytes of the tile's rows or columns; tiles of more than 64 are
 // groups of 64, 8192 bytes apart), whichever way the matrix lies in memory: nothing is ever transposed by hand.
+//
+// kPair: two blocks on neighbouring SMs (a cluster) work on one tile of 256 rows, each with 128 of the rows of A, half the columns of B and the
+// sums of its rows; one of them issues instructions for both.  A block alone moves 48 KB into shared memory and 48 KB out of it for the
+// 512 clocks of a chunk's instructions (128 x 256), 192 bytes a clock where it has 128; in a pair it is 32 and 32.
 //
 // Operands have kParts parts of 16 bits:
 //   1   the operand itself
@@ -32,20 +37,22 @@ using gtc::smem_u32;
 constexpr int kBM = 128, kBK = 64;   // rows of a tile; reduction steps of a chunk
 constexpr int kATile = kBM * kBK * 2;              // bytes of one part of an operand tile of A
 constexpr int kGroup64 = kBK * 128;                // bytes between groups of 64 in an MN-major tile
-constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps, kFirstProducer = kMmaWarp + 1;
+constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps;
 constexpr int kBuffer = 2048;                      // bytes of an epilogue warp's buffer: 32 rows of 64
 
-template <int PARTS, int BN, bool TMA>
+template <int PARTS, int BN, bool TMA, bool PAIR>
 struct Geometry {
-  static constexpr int kBTile = BN * kBK * 2;
+  static constexpr int kBCols = PAIR ? BN / 2 : BN;            // columns of B that this block's shared memory holds
+  static constexpr int kBTile = kBCols * kBK * 2;
   static constexpr int kStage = PARTS * (kATile + kBTile);
   static constexpr int kStages = 196608 / kStage < 8 ? 196608 / kStage : 8;
   static constexpr int kProducers = TMA ? 1 : 8;               // warps
-  static constexpr int kThreads = (kFirstProducer + kProducers) * 32;
+  static constexpr int kThreads = (TMA ? kMmaWarp + 3 : kMmaWarp + kProducers) * 32;
   static constexpr int kAccs = PARTS > 1 ? 2 : 1;              // accumulators of a set
   static constexpr uint32_t kTmemCols = 2 * kAccs * BN;
   static constexpr int kBuffersAt = kStages * kStage, kTablesAt = kBuffersAt + kEpiWarps * kBuffer;
   static_assert(kTmemCols >= 32 && kTmemCols <= 512, "tensor memory");
+  static_assert(!PAIR || (PARTS == 1 && TMA && BN == 256), "the pair has one layout");
 };
 
 // Byte offsets of the 16-byte unit `u` (eight elements) of a tile's row.
@@ -61,10 +68,10 @@ __device__ __forceinline__ uint32_t desc_lo(uint32_t address) { return ((address
 template <bool MN>
 constexpr uint32_t kStep16 = MN ? 2048u >> 4 : 32u >> 4;
 
-// Instruction descriptor: D fp32, A and B both of bf16 or both of fp16, M = 128; N is added per item.
-template <bool A_MN, bool B_MN>
+// Instruction descriptor: D fp32, A and B both of bf16 or both of fp16, M = 128 (of a pair 256); N is added per item.
+template <bool A_MN, bool B_MN, bool PAIR>
 __device__ __forceinline__ uint32_t instruction(bool bf16) {
-  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kBM >> 4) << 24);
+  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)((PAIR ? 2 * kBM : kBM) >> 4) << 24);
 }
 __device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -76,54 +83,136 @@ __device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t
       ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(0u), "r"(kDescHi)
       : "memory");
 }
+// The same for a pair of blocks, M = 256: by one thread of the first block, for both.
+__device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %5};\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      : "memory");
+}
+// Arrives at the barrier of this address in both blocks when all instructions issued so far are done.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+}
+__device__ __forceinline__ uint32_t of_first_block(uint32_t address) {
+  uint32_t there;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(address));
+  return there;
+}
+__device__ __forceinline__ void meet_pair() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// One arrival for the whole warp at a barrier of the pair's first block.  What it orders are reads of tensor memory (tcgen05 fences) or, `wrote`, stores
+// to shared memory that the other block's instructions will read.  (Release and acquire at cluster scope cost hundreds of clocks: with them on every arrival and
+// wait, 32768 x 2048 x 2048 took 540 us instead of 296.)
+__device__ __forceinline__ void arrive_at_first(uint32_t there, bool wrote) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) {
+    if (wrote) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(there) : "memory");
+    else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(there) : "memory");
+  }
+}
+// Announces `bytes` at `bar` and arrives there; where THERE, the first block's.
+template <bool THERE>
+__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
+  if constexpr (THERE) asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+  else asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Copies of a box into this block's shared memory; where PAIR, `bar` may be the first block's.
+template <bool PAIR>
 __device__ __forceinline__ void copy_2d(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(bar)
                : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void copy_3d(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
 
 // What a block needs beside its operands.
 struct Bars {
-  uint64_t full[8], empty[8], acc_full[2], acc_empty[2], drain;
+  uint64_t full[8], empty[8], acc_full[2], acc_empty[2], tail[8], drain;
 };
 
 // NC columns of 32 rows, one row a lane, to `out` (element (0, 0) of the warp's part), the first rows_left rows and cols_left columns of them.
-// Through a buffer, so that what leaves a warp at once are 64 bytes of each of eight rows, whole sectors.  vec: rows of `out` start on 16-byte boundaries.
+// Through a buffer, so that what leaves a warp at once are 64 bytes of each of eight rows, whole sectors.  vec: rows of `out` start on
+// 16-byte boundaries; where they do not, or end inside of 16 bytes, a warp writes 32 columns of a row (fp32) or of two rows at once, halves two by two in whichever way they are
+// aligned (13752 x 767 halves, with its product: 87 us where each lane wrote eight halves one by one, 69 us so).
+__device__ __forceinline__ uint32_t pack(int type, float x, float y) {
+  if (type == kBf16) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&b);
+  }
+  const __half2 b = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
 template <int NC>
 __device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf, void* out, long long ld, int out_type, bool vec, int rows_left, int cols_left) {
   const int lane = threadIdx.x & 31, q = lane & 3;
   uint8_t* const mine = buf + lane * 64;
   const int turn = (lane >> 1) & 3;
-  if (out_type == kF32) {
+  const auto unit = [&](int r, int u) { return buf + r * 64 + ((u ^ ((r >> 1) & 3)) << 4); };
+  const bool wide = out_type == kF32;
+  const int step = wide ? 16 : 32, size = wide ? 4 : 2;   // columns in the buffer at a time
+  const bool whole = vec && rows_left >= 32, quads = vec && (cols_left * size & 15) == 0;
+  // what this lane writes of a row of whole units: unit q of row lane / 4, of that row + 8, ..
+  uint8_t* at = static_cast<uint8_t*>(out) + (lane >> 2) * ld * size + 16 * q;
+  const long long down = 8 * ld * size;
+  const uint8_t* const from = unit(lane >> 2, q);         // rows 8 apart have the same turn: 512 bytes apart
+  const auto leave = [&](int c0) {
+    __syncwarp();
+    if (whole && cols_left - c0 >= step) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
+    } else if (quads) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (8 * i + (lane >> 2) < rows_left && c0 * size + 16 * q < cols_left * size) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
+    } else if (wide) {
+      const int c = lane & 15;
+      for (int r = lane >> 4; r < min(32, rows_left); r += 2)
+        if (c0 + c < cols_left) static_cast<float*>(out)[r * ld + c0 + c] = reinterpret_cast<const float*>(unit(r, c >> 2))[c & 3];
+    } else {
+      // word j of a row holds columns 2 j and 2 j + 1, or, where the row starts in the middle of a word, 2 j - 1 and 2 j: then the first and
+      // the last column of the step go alone
+      const int j = lane & 15, some = cols_left - c0;
+      const auto half = [&](int r, int c) { return (uint32_t)reinterpret_cast<const unsigned short*>(unit(r, c >> 3))[c & 7]; };
+      for (int r = lane >> 4; r < min(32, rows_left); r += 2) {
+        unsigned short* const row = static_cast<unsigned short*>(out) + r * ld + c0;
+        const int c = 2 * j - (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
+        if (c >= 0 && c + 1 < some) *reinterpret_cast<uint32_t*>(row + c) = half(r, c) | half(r, c + 1) << 16;
+        else if (c >= 0 && c < some) row[c] = (unsigned short)half(r, c);
+        else if (c < 0) row[0] = (unsigned short)half(r, 0);
+        if (j == 15 && c < 30 && 31 < some) row[31] = (unsigned short)half(r, 31);
+      }
+    }
+    at += 64;
+    __syncwarp();
+  };
+  if (wide) {
 #pragma unroll
     for (int c0 = 0; c0 < NC; c0 += 16) {
       if (c0 < cols_left) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(mine + ((u ^ turn) << 4)) = make_float4(acc[c0 + 4 * u], acc[c0 + 4 * u + 1], acc[c0 + 4 * u + 2], acc[c0 + 4 * u + 3]);
-        __syncwarp();
-        const int col = c0 + 4 * q, some = cols_left - col;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 8 * i + (lane >> 2);
-          const float4 v = *reinterpret_cast<const float4*>(buf + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
-          float* const at = static_cast<float*>(out) + r * ld + col;
-          if (r < rows_left && some > 0) {
-            if (vec && some >= 4) {
-              *reinterpret_cast<float4*>(at) = v;
-            } else {
-              at[0] = v.x;
-              if (some > 1) at[1] = v.y;
-              if (some > 2) at[2] = v.z;
-              if (some > 3) at[3] = v.w;
-            }
-          }
-        }
-        __syncwarp();
+        leave(c0);
       }
     }
   } else {
@@ -132,53 +221,29 @@ __device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf,
       if (c0 < cols_left) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = acc[c0 + 8 * u + 2 * e], y = acc[c0 + 8 * u + 2 * e + 1];
-            if (out_type == kBf16) {
-              const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
-              w[e] = *reinterpret_cast<const uint32_t*>(&b);
-            } else {
-              const __half2 b = __floats2half2_rn(x, y);
-              w[e] = *reinterpret_cast<const uint32_t*>(&b);
-            }
-          }
-          *reinterpret_cast<uint4*>(mine + ((u ^ turn) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          const float* const x = acc + c0 + 8 * u;
+          *reinterpret_cast<uint4*>(mine + ((u ^ turn) << 4)) =
+              make_uint4(pack(out_type, x[0], x[1]), pack(out_type, x[2], x[3]), pack(out_type, x[4], x[5]), pack(out_type, x[6], x[7]));
         }
-        __syncwarp();
-        const int col = c0 + 8 * q, some = cols_left - col;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 8 * i + (lane >> 2);
-          const uint4 v = *reinterpret_cast<const uint4*>(buf + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
-          unsigned short* const at = static_cast<unsigned short*>(out) + r * ld + col;
-          if (r < rows_left && some > 0) {
-            if (vec && some >= 8) {
-              *reinterpret_cast<uint4*>(at) = v;
-            } else {
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (e < some) at[e] = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
-            }
-          }
-        }
-        __syncwarp();
+        leave(c0);
       }
     }
   }
 }
 
-// Eight elements of a row on their way from memory to an operand tile, those from `valid` on zero.  vec: the row's units are 16-byte aligned.
+// Eight elements of a row on their way from memory to an operand tile, those from `valid` on zero.
 template <typename T>
 struct Raw;
 template <>
 struct Raw<float> {
   float x[8];
-  __device__ __forceinline__ void load(const float* p, int valid, bool vec) {
-    if (vec && valid >= 8) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  // VEC: quads are 16-byte aligned and lie inside or outside as a whole
+  template <bool VEC>
+  __device__ __forceinline__ void load(const float* p, int valid) {
+    if constexpr (VEC) {
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+      if (valid > 0) a = __ldg(reinterpret_cast<const float4*>(p));
+      if (valid > 4) b = __ldg(reinterpret_cast<const float4*>(p) + 1);
       x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     } else {
 #pragma unroll
@@ -205,32 +270,36 @@ struct Raw<float> {
 template <>
 struct Raw<unsigned short> {
   uint4 x;
-  __device__ __forceinline__ void load(const unsigned short* p, int valid, bool vec) {
-    if (vec && valid >= 8) {
-      x = __ldg(reinterpret_cast<const uint4*>(p));
-    } else {
-      uint32_t w[4];
+  template <bool>
+  __device__ __forceinline__ void load(const unsigned short* p, int valid) {
+    uint32_t w[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        w[e] = (2 * e < valid ? (uint32_t)__ldg(p + 2 * e) : 0u) | (2 * e + 1 < valid ? (uint32_t)__ldg(p + 2 * e + 1) << 16 : 0u);
-      x = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int e = 0; e < 4; ++e)
+      w[e] = (2 * e < valid ? (uint32_t)__ldg(p + 2 * e) : 0u) | (2 * e + 1 < valid ? (uint32_t)__ldg(p + 2 * e + 1) << 16 : 0u);
+    x = make_uint4(w[0], w[1], w[2], w[3]);
   }
   __device__ __forceinline__ void store(uint8_t* at, int) const { *reinterpret_cast<uint4*>(at) = x; }
 };
 
 // The shared loop.  A job J says what the items are, where operand tiles come from and what becomes of a tile's sums:
-//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kSegment (chunks), kMeets (finish() has barriers of the epilogue warps)
-//   J(args, tables)                   built by every thread; setup(): tables in shared memory, by the whole block, between barriers
-//   bool item(unsigned i, Item&)      the i-th item, false behind the last; Item has chunks (of the reduction, maybe none), n (columns) and tail
+//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kPair, kSegment (chunks), kMeets (finish() has barriers of the epilogue warps)
+//   J(args, tables, rank)             built by every thread (rank: of the block in its pair); setup(): tables in shared memory, by the whole
+//                                     block, between barriers
+//   J::Walk start(worker, workers)    where this block's (pair's) items begin
+//   bool next(Walk&, Item&)           the next of them, false behind the last; Item has chunks (of the reduction, maybe none), n (columns) and tail
 //                                     (steps of the last chunk that count, where rows behind them hold other data; else 64)
-//   copy(item, chunk, tile, bar)      kTma: issues the copies of a chunk and announces their bytes
-//   load(item, chunk, thread, raw_a, raw_b)   otherwise
+//   copy(item, chunk, tile, bar)      kTma: announces the bytes of this block's copies of a chunk at `bar` and issues them; template argument: whether `bar` is
+//                                     the first block's
+//   load_a, load_b(item, chunk, unit, raw)   otherwise: eight elements of a tile
 //   finish(item, acc, buf, warp)      the sums of this warp's rows and columns; by all epilogue warps
 template <class J>
-__global__ void __launch_bounds__(Geometry<J::kParts, J::kBN, J::kTma>::kThreads, 1) k_products(const __grid_constant__ typename J::Args args) {
-  using G = Geometry<J::kParts, J::kBN, J::kTma>;
+using GeometryOf = Geometry<J::kParts, J::kBN, J::kTma, J::kPair>;
+
+template <class J>
+__global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const __grid_constant__ typename J::Args args) {
+  using G = GeometryOf<J>;
   constexpr int S = G::kStages, BN = J::kBN, PARTS = J::kParts, kSegment = J::kSegment;
+  constexpr bool PAIR = J::kPair;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) Bars bars;
   __shared__ uint32_t tmem_slot;
@@ -239,135 +308,198 @@ __global__ void __launch_bounds__(Geometry<J::kParts, J::kBN, J::kTma>::kThreads
   const uint32_t base = smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), acc_full = smem_u32(bars.acc_full), acc_empty = smem_u32(bars.acc_empty);
+  const uint32_t drain = smem_u32(&bars.drain), tail = smem_u32(bars.tail);
+  // of the pair: its first block (rank 0) issues the instructions, and the barriers that it waits on for both are its own
+  const int rank = PAIR ? (int)(blockIdx.x & 1) : 0;
+  const unsigned worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
+  const uint32_t full_there = PAIR ? of_first_block(full) : full, acc_empty_there = PAIR ? of_first_block(acc_empty) : acc_empty;
   if (tid == 0) {
     for (int s = 0; s < S; ++s) {
-      gtc::mbar_init(full + 8 * s, G::kProducers);
+      gtc::mbar_init(full + 8 * s, PAIR ? 2 : G::kProducers);
       gtc::mbar_init(empty + 8 * s, 1);
+      gtc::mbar_init(tail + 8 * s, 1);
     }
     for (int a = 0; a < 2; ++a) {
       gtc::mbar_init(acc_full + 8 * a, 1);
-      gtc::mbar_init(acc_empty + 8 * a, kEpiWarps);
+      gtc::mbar_init(acc_empty + 8 * a, PAIR ? 2 * kEpiWarps : kEpiWarps);
     }
-    gtc::mbar_init(smem_u32(&bars.drain), 1);
+    gtc::mbar_init(drain, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(G::kTmemCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(G::kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(G::kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   gtc::enter_kernel();
-  J job(args, smem + G::kTablesAt);
+  J job(args, smem + G::kTablesAt, rank);
   job.setup();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if constexpr (PAIR) meet_pair();   // both blocks' barriers are there
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
   volatile int* const abortp = &abort_flag;
   int copies = 0;   // stages this thread has started copies into
   typename J::Item it;
+  typename J::Walk walk = job.start(worker, workers);
 
-  if (warp >= kFirstProducer) {
+  // Issues the instructions of a chunk and what announces their end; by one thread.
+  const uint32_t kind = instruction<J::kAMn, J::kBMn, PAIR>(job.bf16());
+  const auto issue = [&](int slot, int set, int columns, int steps, bool first, bool ends) {
+    const uint32_t at = base + (uint32_t)slot * G::kStage, idesc = kind | (uint32_t)((PAIR ? BN : (min(columns, BN) + 15) / 16 * 16) >> 3) << 17;
+    const uint32_t a = desc_lo<J::kAMn>(at), b = desc_lo<J::kBMn>(at + PARTS * kATile);
+    constexpr uint32_t pa = kATile >> 4, pb = G::kBTile >> 4, oa = kStep16<J::kAMn>, ob = kStep16<J::kBMn>;
+    const uint32_t d = tmem + (uint32_t)(set * G::kAccs * BN);
+    for (int k = 0; k < steps; ++k) {
+      const uint32_t ak = a + k * oa, bk = b + k * ob, go_on = !first || k > 0;
+      if constexpr (PAIR) {
+        mma_pair(d, ak, bk, idesc, go_on);
+      } else {
+        mma(d, ak, bk, idesc, go_on);
+        if constexpr (PARTS > 1) {
+          mma(d + BN, ak, bk + pb, idesc, go_on);
+          mma(d + BN, ak + pa, bk, idesc, 1u);
+        }
+        if constexpr (PARTS > 2) {
+          mma(d + BN, ak + pa, bk + pb, idesc, 1u);
+          mma(d + BN, ak, bk + 2 * pb, idesc, 1u);
+          mma(d + BN, ak + 2 * pa, bk, idesc, 1u);
+        }
+      }
+    }
+    if constexpr (PAIR) {
+      commit_pair(empty + 8 * slot);
+      if (ends) commit_pair(acc_full + 8 * set);
+    } else {
+      gtc::mma_commit(empty + 8 * slot);
+      if (ends) gtc::mma_commit(acc_full + 8 * set);
+    }
+  };
+
+  if (warp == kMmaWarp + 2 && J::kTma) {
+    if constexpr (J::kTma && J::kAMn) {
+      // Rows of the next group come with the last chunk of a tile: the steps that are still read are cleared in both operands, in a pair by each
+      // block in its own.  A warp of its own does it while chunks before this one are multiplied, and then arrives where
+      // copies of other chunks arrive.  (Where the issuing warp did it, chunks behind waited.)
+      int slot = 0;
+      uint32_t parities = 0;   // of the slots, a bit each
+      bool ok = true;
+      while (ok && job.next(walk, it)) {
+        slot = (slot + it.chunks) % S;
+        if (it.chunks == 0 || it.tail == kBK) continue;
+        const int at = (slot + S - 1) % S, steps = (it.tail + 15) / 16, clear = steps * 16 - it.tail, groups = kBM / 64 + G::kBCols / 64;
+        ok = __all_sync(0xffffffffu, gtc::mbar_wait_abortable(tail + 8 * at, parities >> at & 1u, abortp));
+        if (!ok) break;
+        parities ^= 1u << at;
+        for (int u = lane; u < clear * groups * 8; u += 32) {
+          const int row = it.tail + (u >> 3) % clear, group = (u >> 3) / clear;
+          *reinterpret_cast<uint4*>(smem + (size_t)at * G::kStage + group * kGroup64 + row * 128 + (u & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if constexpr (PAIR) arrive_at_first(full_there + 8 * at, true);
+        else gtc::mbar_arrive_warp(full + 8 * at);
+      }
+    }
+  } else if (warp == kMmaWarp + 1 && J::kTma) {
     int slot = 0;
     uint32_t parity = 1;   // a fresh barrier passes a wait on parity 1
     if constexpr (J::kTma) {
       if (lane == 0) {
         bool ok = true;
-        for (unsigned i = blockIdx.x; ok && job.item(i, it); i += gridDim.x) {
+        while (ok && job.next(walk, it)) {
           for (int c = 0; c < it.chunks; ++c) {
             ok = gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp);
             if (!ok) break;
-            job.copy(it, c, base + (uint32_t)slot * G::kStage, full + 8 * slot);
+            const uint32_t tile = base + (uint32_t)slot * G::kStage;
+            // a chunk with rows to clear is announced to the warp that does it
+            if (J::kAMn && it.tail < kBK && c + 1 == it.chunks) job.template copy<false>(it, c, tile, tail + 8 * slot);
+            else job.template copy<PAIR>(it, c, tile, full_there + 8 * slot);
             ++copies;
             if (++slot == S) { slot = 0; parity ^= 1u; }
           }
         }
       }
-    } else {
+    }
+  } else if (warp >= kMmaWarp && !J::kTma) {
+    if constexpr (!J::kTma) {
       using R = Raw<typename J::T>;
       R a[kBM * 8 / 256], b[BN * 8 / 256];
-      const int t = tid - kFirstProducer * 32;
-      unsigned i = blockIdx.x;
-      int c = 0;
-      bool more = job.item(i, it);
+      const int t = tid - kMmaWarp * 32;
+      int slot = 0, set = 0, c = 0;
+      uint32_t parity = 1, acc_parity = 1;
+      bool more = job.next(walk, it);
       const auto settle = [&] {   // on to the next item where this one has no chunk left
         while (more && c >= it.chunks) {
-          i += gridDim.x;
           c = 0;
-          more = job.item(i, it);
+          more = job.next(walk, it);
         }
       };
       settle();
-      if (more) job.load(it, c, t, a, b);
+      if (more) {
+#pragma unroll
+        for (int u = 0; u < kBM * 8 / 256; ++u) job.load_a(it, c, t + 256 * u, a[u]);
+#pragma unroll
+        for (int u = 0; u < BN * 8 / 256; ++u) job.load_b(it, c, t + 256 * u, b[u]);
+      }
       while (more) {
         if (!__all_sync(0xffffffffu, gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp))) break;
         uint8_t* const st = smem + (size_t)slot * G::kStage;
+        const bool first = c % kSegment == 0, ends = c + 1 == it.chunks || c % kSegment == kSegment - 1;
+        const int columns = it.n;
+        ++c;
+        settle();
+        // eight elements go to shared memory and those of the next chunk into their place: loads are on their way during all of this
 #pragma unroll
         for (int u = 0; u < kBM * 8 / 256; ++u) {
           const int at = t + 256 * u;
           a[u].store(st + (J::kAMn ? unit_mn(at / (kBM / 8), at % (kBM / 8)) : unit_k(at >> 3, at & 7)), kATile);
+          if (more) job.load_a(it, c, at, a[u]);
         }
 #pragma unroll
         for (int u = 0; u < BN * 8 / 256; ++u) {
           const int at = t + 256 * u;
           b[u].store(st + PARTS * kATile + (J::kBMn ? unit_mn(at / (BN / 8), at % (BN / 8)) : unit_k(at >> 3, at & 7)), G::kBTile);
+          if (more) job.load_b(it, c, at, b[u]);
         }
-        ++c;
-        settle();
-        if (more) job.load(it, c, t, a, b);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         gtc::mbar_arrive_warp(full + 8 * slot);
+        if (warp == kMmaWarp) {   // the others are about as far
+          if (!__all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
+                                           gtc::mbar_wait_abortable(full + 8 * slot, parity ^ 1u, abortp)))
+            break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          if (lane == 0) issue(slot, set, columns, kBK / 16, first, ends);
+          __syncwarp();
+          if (ends) {
+            if (set == 1) acc_parity ^= 1u;
+            set ^= 1;
+          }
+        }
         if (++slot == S) { slot = 0; parity ^= 1u; }
       }
     }
   } else if (warp == kMmaWarp) {
-    const uint32_t kind = instruction<J::kAMn, J::kBMn>(job.bf16());
     int slot = 0, set = 0;
     uint32_t parity = 0, acc_parity = 1;
-    bool ok = true;
-    for (unsigned i = blockIdx.x; ok && job.item(i, it); i += gridDim.x) {
-      const uint32_t idesc = kind | (uint32_t)((min(it.n, BN) + 15) / 16 * 2) << 17;
+    bool ok = rank == 0;
+    while (ok && job.next(walk, it)) {
       for (int c = 0; c < it.chunks; ++c) {
-        const bool first = c % kSegment == 0, last = c + 1 == it.chunks;
+        const bool first = c % kSegment == 0, last = c + 1 == it.chunks, ends = last || c % kSegment == kSegment - 1;
+        const bool clears = J::kAMn && last && it.tail < kBK;
         ok = __all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
                                          gtc::mbar_wait_abortable(full + 8 * slot, parity, abortp));
         if (!ok) break;
-        const uint32_t at = base + (uint32_t)slot * G::kStage;
-        int steps = kBK / 16;
-        if (J::kTma && J::kAMn && last && it.tail < kBK) {
-          // rows of the next group came with the copy: the steps that are still read are cleared in both operands
-          steps = (it.tail + 15) / 16;
-          const int clear = steps * 16 - it.tail, groups = kBM / 64 + BN / 64;
-          for (int u = lane; u < clear * groups * 8; u += 32) {
-            const int row = it.tail + (u >> 3) % clear, group = (u >> 3) / clear;
-            *reinterpret_cast<uint4*>(smem + (size_t)slot * G::kStage + group * kGroup64 + row * 128 + (u & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-        }
+        if (PAIR && clears) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the other block's stores
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (lane == 0) {
-          const uint32_t a = desc_lo<J::kAMn>(at), b = desc_lo<J::kBMn>(at + PARTS * kATile);
-          constexpr uint32_t pa = kATile >> 4, pb = G::kBTile >> 4, oa = kStep16<J::kAMn>, ob = kStep16<J::kBMn>;
-          const uint32_t d = tmem + (uint32_t)(set * G::kAccs * BN);
-          for (int k = 0; k < steps; ++k) {
-            const uint32_t ak = a + k * oa, bk = b + k * ob, go_on = !first || k > 0;
-            mma(d, ak, bk, idesc, go_on);
-            if constexpr (PARTS > 1) {
-              mma(d + BN, ak, bk + pb, idesc, go_on);
-              mma(d + BN, ak + pa, bk, idesc, 1u);
-            }
-            if constexpr (PARTS > 2) {
-              mma(d + BN, ak + pa, bk + pb, idesc, 1u);
-              mma(d + BN, ak, bk + 2 * pb, idesc, 1u);
-              mma(d + BN, ak + 2 * pa, bk, idesc, 1u);
-            }
-          }
-          gtc::mma_commit(empty + 8 * slot);
-          if (last || c % kSegment == kSegment - 1) gtc::mma_commit(acc_full + 8 * set);
-        }
+        if (lane == 0) issue(slot, set, it.n, clears ? (it.tail + 15) / 16 : kBK / 16, first, ends);
         __syncwarp();
-        if (last || c % kSegment == kSegment - 1) {
+        if (ends) {
           if (set == 1) acc_parity ^= 1u;
           set ^= 1;
         }
@@ -382,7 +514,7 @@ __global__ void __launch_bounds__(Geometry<J::kParts, J::kBN, J::kTma>::kThreads
     int set = 0;
     uint32_t parity = 0;
     bool ok = true;
-    for (unsigned i = blockIdx.x; ok && job.item(i, it); i += gridDim.x) {
+    while (ok && job.next(walk, it)) {
       float acc[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) acc[c] = 0.f;
@@ -393,18 +525,29 @@ __global__ void __launch_bounds__(Geometry<J::kParts, J::kBN, J::kTma>::kThreads
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (mine) {
           const uint32_t from = lanes + (uint32_t)(set * G::kAccs * BN);
+          // 16 columns are added while the next 16 are on their way
+          uint32_t v[2][16], w[PARTS > 1 ? 2 : 1][16];
+          GTC_TMEM_LD16(v[0], from);
+          if constexpr (PARTS > 1) GTC_TMEM_LD16(w[0], from + BN);
 #pragma unroll
           for (int c0 = 0; c0 < NC; c0 += 16) {
-            uint32_t v[16], w[16];
-            GTC_TMEM_LD16(v, from + c0);
-            if (PARTS > 1) GTC_TMEM_LD16(w, from + BN + c0);
+            constexpr int kLast = NC - 16;
+            const int now = c0 / 16 & 1;
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            if (c0 < kLast) {
+              GTC_TMEM_LD16(v[now ^ 1], from + c0 + 16);
+              if constexpr (PARTS > 1) GTC_TMEM_LD16(w[now ^ 1], from + BN + c0 + 16);
+            }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[c0 + e] += PARTS > 1 ? fmaf(__uint_as_float(w[e]), kCorrection, __uint_as_float(v[e])) : __uint_as_float(v[e]);
+            for (int e = 0; e < 16; ++e) {
+              if constexpr (PARTS > 1) acc[c0 + e] += fmaf(__uint_as_float(w[now][e]), kCorrection, __uint_as_float(v[now][e]));
+              else acc[c0 + e] += __uint_as_float(v[now][e]);
+            }
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        gtc::mbar_arrive_warp(acc_empty + 8 * set);
+        if constexpr (PAIR) arrive_at_first(acc_empty_there + 8 * set, false);
+        else gtc::mbar_arrive_warp(acc_empty + 8 * set);
         if (set == 1) parity ^= 1u;
         set ^= 1;
       }
@@ -417,13 +560,22 @@ __global__ void __launch_bounds__(Geometry<J::kParts, J::kBN, J::kTma>::kThreads
   __syncthreads();
   if (abort_flag) {   // what is still in flight is waited for before shared and tensor memory are let go
     if (tid == 0) atomicOr(job.error_flag(), 1);
-    if (warp == kFirstProducer && lane == 0 && J::kTma) gtc::drain_copies(full, S, copies);
-    if (warp == kMmaWarp && lane == 0) gtc::drain_mmas(smem_u32(&bars.drain));
+    if (warp == kMmaWarp + 1 && lane == 0 && J::kTma && rank == 0) gtc::drain_copies(full, S, copies);
+    if (warp == kMmaWarp && lane == 0 && rank == 0) {
+      if constexpr (PAIR) {
+        commit_pair(drain);
+        gtc::drain_wait(drain, 0);
+      } else {
+        gtc::drain_mmas(drain);
+      }
+    }
     __syncthreads();
   }
+  if constexpr (PAIR) meet_pair();   // neither block's memory is used by the other any more
   if (warp == kMmaWarp) {
     __syncwarp();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::kTmemCols) : "memory");
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::kTmemCols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::kTmemCols) : "memory");
   }
 }
 

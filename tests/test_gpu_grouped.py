@@ -173,6 +173,32 @@ def test_larger_ones(h, kind):
     run_tn(h, [40] * 200, 24, 40, kind, "f32")
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_tiles_of_256_by_256(h, kind):
+    """Widths that fill them and enough rows for all SMs: ends of groups at every place of a tile, idle groups, sums of one chunk and of many."""
+    rng = np.random.default_rng(2)
+    sizes = np.concatenate([rng.integers(0, 700, 40), [0, 1, 63, 64, 65, 255, 256, 257, 0]])
+    for k, n in ((8, 512), (200, 250), (328, 1016)):
+        run_product(h, sizes, k, n, kind, kind, first=3, tail=5)
+        run_product(h, sizes, k, n, kind, "f32", transposed=True, first=3, tail=5)
+    few = rng.integers(0, 64, 200)
+    for ka, nb in ((256, 256), (248, 504), (1000, 232)):
+        run_tn(h, sizes, ka, nb, kind, "f32", first=3, tail=5)
+        run_tn(h, sizes, ka, nb, kind, kind)
+    run_tn(h, few, 256, 248, kind, "f32")
+    run_tn(h, [30000, 0, 1, 777], 512, 256, kind, "f32")
+    run_tn(h, [0, 0], 256, 256, kind, kind)
+
+
+@pytest.mark.parametrize("kind", NAMES)
+def test_sums_shared_by_many_blocks(h, kind):
+    """Few tiles and many rows: a tile's sum comes from up to all blocks of the chip; equal and very unequal groups."""
+    run_tn(h, [50001], 40, 24, kind, "f32")
+    run_tn(h, [30000, 1, 0, 7000], 136, 72, kind, kind)
+    run_tn(h, [64 * 37] * 9, 64, 264, kind, "f32")
+    run_tn(h, [0, 0, 25000], 130, 7, kind, "f32")
+
+
 def test_most_groups(h):
     sizes = np.arange(1024) % 3
     run_product(h, sizes, 24, 16, "bf16", "bf16")
