@@ -382,9 +382,12 @@ struct ProductTnJob {
 };
 
 // ---- orthogonalised updates --------------------------------------------------------------------------
-// X <- P X with P = a I + b S + c S S, S = X X^T; for matrices taller than wide X <- X P with S = X^T X.  Three products a step, all by pairs
-// of halves (three matrix instructions for one, 22 bits of each operand): single halves, at 11 bits, end 1e-3 off, more than a bf16 result may lose, and
-// 4e-2 where singular values span four decades, since the steps lift the small ones, and what they are off, by |a| each.
+// X <- P X with P = a I + b S + c S S, S = X X^T; for matrices taller than wide X <- X P with S = X^T X.  Three products a step, in two forms.
+//  2 parts: pairs of halves (three matrix instructions for one, 22 bits of each operand), for results of fp32 and fp16.
+//  1 part: operands are halves, but what is large is kept out of them: the diagonals of S and P stay in fp32 (S S of the rest O is
+//    O O + (D_i + D_j) O_ij), and X, a pair of halves, is itself multiplied by a + P_ii in fp32.  For results of bf16, whose
+//    rounding is 1.7e-3 of the result: five steps end 0.5 to 0.8e-3 off (1.3e-3 where 280 of 300 singular values are 1e-3 of the rest), in a third of the
+//    instructions.  With the diagonals inside it is 1.3 to 1.8e-3, with X in halves only 1e-3 to 4e-2: the steps lift small singular values, and what they are off, by |a| each.
 // Matrices between products are images: part hi of all matrices, then part lo, rows padded to 16 bytes, under a power of two that comes from
 // the bounds of the singular values (host, grow()): entries stay below 2^15 and far above the smallest half.  S and P are symmetric: only
 // tiles that reach the diagonal are formed, the others are written turned.  X keeps its own orientation throughout, so nothing is transposed.
@@ -470,8 +473,11 @@ struct OrthogonalArgs {
   int* error_flag;
   int batch, rows, cols, k;     // of the products: D is rows x cols, the reduction has k steps
   float factor;                 // of the sums, for what is stored
-  float diagonal, linear;       // kPolynomial: a under the scale of P, b over the scale of S times that of P
-  Image s, to;                  // kPolynomial: S; where the result goes
+  float diagonal, linear;       // kPolynomial: a, under the scale of P where it is in P; b under that of P over that of S.  kMove: the scale of the result over that of X
+  Image s, to;                  // kPolynomial: S, kMove: X; where the result goes
+  const float* diagonals;       // 1 part, kPolynomial: of S (under its scale), kMove: a + those of P
+  float* to_diagonals;          // 1 part: where those of the result go
+  float unscale;                // 1 part, kPolynomial: one over the scale of P
   void* out;                    // last kMove: the caller's matrix
   int out_type;
   long long ldo, stride_o;
@@ -510,23 +516,26 @@ __device__ __forceinline__ void store_turned(const float (&acc)[NC], uint8_t* bu
   }
 }
 
-template <Stage STAGE, int BN, bool A_MN, bool B_MN>
+template <Stage STAGE, int PARTS, int BN, bool A_MN, bool B_MN, bool PAIR>
 struct OrthogonalJob {
   using Args = OrthogonalArgs;
-  static constexpr int kParts = 2, kBN = BN, kSegment = 1;
-  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kPair = false, kSymmetric = STAGE != kMove;
+  static constexpr int kParts = PARTS, kBN = BN, kSegment = PARTS == 1 ? 4 : 1;   // pairs are for results that show where sums are cut
+  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
+  static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kBCols = PAIR ? BN / 2 : BN;
   struct Item {
     int chunks, n, tail, matrix, row0, col0;
+    bool turn;
   };
   const Args& a;
-  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int) : a(args) {}
+  int rank;
+  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int rank_) : a(args), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return false; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {}
-  // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kBM / BN (i + 1)
+  // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kTileRows / BN (i + 1)
   __host__ __device__ static long long tiles(int rows, int cols) {
-    const long long m = (rows + kBM - 1) / kBM;
-    return kSymmetric ? kBM / BN * (m * (m + 1) / 2) : m * ((cols + BN - 1) / BN);
+    const long long m = (rows + kTileRows - 1) / kTileRows;
+    return kSymmetric ? kTileRows / BN * (m * (m + 1) / 2) : m * ((cols + BN - 1) / BN);
   }
   struct Walk {
     unsigned i, step;
@@ -540,18 +549,20 @@ struct OrthogonalJob {
     const unsigned t = i - (unsigned)it.matrix * per;
     unsigned row, col;
     if constexpr (kSymmetric) {
-      const unsigned u = t / (kBM / BN);   // in blocks of kBM columns
+      constexpr unsigned kAcross = kTileRows / BN;
+      const unsigned u = t / kAcross;   // in blocks of kTileRows columns
       row = (unsigned)((sqrtf(8.f * (float)u + 1.f) - 1.f) * 0.5f);
       while (row * (row + 1) / 2 > u) --row;
       while ((row + 1) * (row + 2) / 2 <= u) ++row;
-      col = t - kBM / BN * (row * (row + 1) / 2);
+      col = t - kAcross * (row * (row + 1) / 2);
     } else {
       const unsigned across = (unsigned)((a.cols + BN - 1) / BN);
       row = t / across;
       col = t - row * across;
     }
-    it.row0 = (int)row * kBM;
     it.col0 = (int)col * BN;
+    it.turn = kSymmetric && it.col0 + BN <= (int)row * kTileRows;
+    it.row0 = (int)row * kTileRows + rank * kBM;
     it.n = a.cols - it.col0;
     it.chunks = it.n > 0 ? (a.k + kBK - 1) / kBK : 0;   // (a symmetric matrix's last row block may reach past its columns)
     it.tail = kBK;
@@ -559,22 +570,41 @@ struct OrthogonalJob {
   }
   template <bool THERE>
   __device__ __forceinline__ void copy(const Item& it, int c, uint32_t tile, uint32_t bar) const {
-    constexpr int kBTile = BN * kBK * 2;
-    const int boxes_a = A_MN ? min(kBM / 64, (a.rows - it.row0 + 63) / 64) : kBM / 64, boxes_b = B_MN ? min(BN / 64, (it.n + 63) / 64) : BN / 64;
-    expect<THERE>(bar, (uint32_t)(2 * (boxes_a + boxes_b) * kGroup64));
+    constexpr int kBTile = kBCols * kBK * 2;
+    const int col0 = it.col0 + rank * kBCols;
+    const int boxes_a = A_MN ? min(kBM / 64, max(0, (a.rows - it.row0 + 63) / 64)) : kBM / 64, boxes_b = B_MN ? min(kBCols / 64, max(0, (a.cols - col0 + 63) / 64)) : kBCols / 64;
+    expect<THERE>(bar, (uint32_t)(PARTS * (boxes_a + boxes_b) * kGroup64));
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
+    for (int part = 0; part < PARTS; ++part) {
       const int z = part * a.batch + it.matrix;
-      const uint32_t ta = tile + part * kATile, tb = tile + 2 * kATile + part * kBTile;
+      const uint32_t ta = tile + part * kATile, tb = tile + PARTS * kATile + part * kBTile;
       if constexpr (A_MN) {
         for (int b = 0; b < boxes_a; ++b) copy_3d<THERE>(ta + b * kGroup64, &a.a, it.row0 + 64 * b, c * kBK, z, bar);
       } else {
         copy_3d<THERE>(ta, &a.a, c * kBK, it.row0, z, bar);
       }
       if constexpr (B_MN) {
-        for (int b = 0; b < boxes_b; ++b) copy_3d<THERE>(tb + b * kGroup64, &a.b, it.col0 + 64 * b, c * kBK, z, bar);
+        for (int b = 0; b < boxes_b; ++b) copy_3d<THERE>(tb + b * kGroup64, &a.b, col0 + 64 * b, c * kBK, z, bar);
       } else {
-        copy_3d<THERE>(tb, &a.b, c * kBK, it.col0, z, bar);
+        copy_3d<THERE>(tb, &a.b, c * kBK, col0, z, bar);
+      }
+    }
+  }
+  // f(column, hi, lo) for the elements of a row of an image, eight at a time (rows are padded to that); LO: whether lo is there.
+  template <int NC, bool LO, typename F>
+  __device__ __forceinline__ static void for_row(const Image& im, const __half* at, int cols_left, const F& f) {
+#pragma unroll
+    for (int c0 = 0; c0 < NC; c0 += 8) {
+      asm volatile("" ::: "memory");   // one unit at a time: all loads at once do not fit the registers
+      if (c0 < cols_left) {
+        const uint4 hi = *reinterpret_cast<const uint4*>(at + c0), lo = LO ? *reinterpret_cast<const uint4*>(at + im.part + c0) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
+          f(c0 + 2 * e, LO ? fmaf(y.x, 0x1p-11f, x.x) : x.x);
+          f(c0 + 2 * e + 1, LO ? fmaf(y.y, 0x1p-11f, x.y) : x.y);
+        }
       }
     }
   }
@@ -583,26 +613,46 @@ struct OrthogonalJob {
     const int row0 = it.row0 + (warp & 3) * 32, col0 = it.col0 + (warp >> 2) * NC, row = row0 + (threadIdx.x & 31);
     const int rows_left = a.rows - row0, cols_left = a.cols - col0;
     if (rows_left <= 0 || cols_left <= 0) return;
+    const int own = min(row, a.rows - 1);   // a row that exists
+    const bool diagonal = kSymmetric && row0 < col0 + NC && col0 < row0 + 32;   // whether the warp holds some of it
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[c] *= a.factor;
     if constexpr (STAGE == kPolynomial) {
-      const __half* const s = a.s.matrix(it.matrix) + (long long)min(row, a.rows - 1) * a.s.ld + col0;
+      const __half* const s = a.s.matrix(it.matrix) + (long long)own * a.s.ld + col0;
+      if constexpr (PARTS == 2) {
+        for_row<NC, true>(a.s, s, cols_left, [&](int c, float x) { acc[c] = fmaf(a.linear, x, acc[c]); });
+        if (diagonal) {
 #pragma unroll
-      for (int c0 = 0; c0 < NC; c0 += 8) {
-        if (c0 < cols_left) {   // rows of an image are padded to eight elements
-          const uint4 hi = *reinterpret_cast<const uint4*>(s + c0), lo = *reinterpret_cast<const uint4*>(s + a.s.part + c0);
-          const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+          for (int c = 0; c < NC; ++c)
+            if (row == col0 + c) acc[c] += a.diagonal;
+        }
+      } else {
+        const float* const d = a.diagonals + (long long)it.matrix * a.rows;
+        const float mine = d[own];
+        // acc is c O O under the scale of P: with the diagonals of S, b O + c (O O + (D_i + D_j) O); on the diagonal b D + c (O O + D D)
+        for_row<NC, false>(a.s, s, cols_left, [&](int c, float x) { acc[c] = fmaf(x, fmaf(a.factor, mine + d[min(col0 + c, a.cols - 1)], a.linear), acc[c]); });
+        if (diagonal) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
-            acc[c0 + 2 * e] = fmaf(a.linear, fmaf(y.x, 0x1p-11f, x.x), acc[c0 + 2 * e]);
-            acc[c0 + 2 * e + 1] = fmaf(a.linear, fmaf(y.y, 0x1p-11f, x.y), acc[c0 + 2 * e + 1]);
-          }
+          for (int c = 0; c < NC; ++c)
+            if (row == col0 + c) acc[c] = fmaf(mine, fmaf(a.factor, mine, a.linear), acc[c]);
         }
       }
+    }
+    if (PARTS == 1 && diagonal) {
+      float* const to = a.to_diagonals + (long long)it.matrix * a.rows;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
-        if (row == col0 + c) acc[c] += a.diagonal;
+        if (row == col0 + c) {
+          if (row < a.rows) to[row] = STAGE == kPolynomial ? fmaf(acc[c], a.unscale, a.diagonal) : acc[c];
+          acc[c] = 0.f;
+        }
+    }
+    if constexpr (PARTS == 1 && STAGE == kMove) {
+      constexpr bool kTall = !B_MN;
+      const float* const d = a.diagonals + (long long)it.matrix * (kTall ? a.cols : a.rows);
+      const float by_row = kTall ? 0.f : d[own] * a.linear;
+      const __half* const x = a.s.matrix(it.matrix) + (long long)own * a.s.ld + col0;
+      for_row<NC, true>(a.s, x, cols_left, [&](int c, float v) { acc[c] = fmaf(v, kTall ? d[min(col0 + c, a.cols - 1)] * a.linear : by_row, acc[c]); });
     }
     if (STAGE == kMove && a.out != nullptr) {
       const long long at = (long long)it.matrix * a.stride_o + row0 * a.ldo + col0;
@@ -611,14 +661,15 @@ struct OrthogonalJob {
       return;
     }
     __half* const to = a.to.matrix(it.matrix);
-    const bool turn = kSymmetric && it.col0 + BN <= it.row0;
     // images have room up to their leading dimension, and whole units there
     store_rows<NC>(acc, buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
-    if (turn) store_turned<NC>(acc, buf, to + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+    if (it.turn) store_turned<NC>(acc, buf, to + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+    if constexpr (PARTS == 2 || STAGE == kMove) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = (acc[c] - __half2float(__float2half_rn(acc[c]))) * 0x1p11f;
-    store_rows<NC>(acc, buf, to + a.to.part + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
-    if (turn) store_turned<NC>(acc, buf, to + a.to.part + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+      for (int c = 0; c < NC; ++c) acc[c] = (acc[c] - __half2float(__float2half_rn(acc[c]))) * 0x1p11f;
+      store_rows<NC>(acc, buf, to + a.to.part + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
+      if (it.turn) store_turned<NC>(acc, buf, to + a.to.part + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+    }
   }
 };
 
@@ -735,6 +786,7 @@ std::size_t tickets_of(const ProductTn& p) { return 3ull * plan(p).grid; }
 struct OrthogonalSpace {
   double* partial;
   Image x[2], s, p;
+  float *s_diagonals, *p_diagonals;
   std::size_t bytes;
   OrthogonalSpace(const Orthogonal& o, void* space) {
     const int m = std::min(o.rows, o.cols);
@@ -754,6 +806,8 @@ struct OrthogonalSpace {
     x[1] = image(o.rows, o.cols);
     s = image(m, m);
     p = image(m, m);
+    s_diagonals = static_cast<float*>(take((std::size_t)o.batch * m * sizeof(float)));
+    p_diagonals = static_cast<float*>(take((std::size_t)o.batch * m * sizeof(float)));
     bytes = used;
   }
 };
@@ -852,15 +906,20 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
     e = launch_plain(k_start<decltype(in), decltype(out)>, dim3((unsigned)std::min<long long>(1024, cdiv(elements, 2048)), (unsigned)p.batch), room, p, at.partial, partials,
                      p.steps > 0 ? at.x[0] : none, (float)scale);
   });
+  const bool halves = p.out_type == kBf16;   // one part is enough
   const auto map = [&](CUtensorMap* t, const Image& im, int cols, int box_rows) {
     return make_map(t, kF16, im.at, cols, im.rows, im.ld, 2LL * p.batch, (long long)im.rows * im.ld, box_rows);
   };
+  // Pairs of SMs where they all get a tile of 256 x 256, else the widest tile of 128 rows that every SM gets one of
+  const auto triangle = [&](int rows) { return p.batch * (cdiv(m, rows) * (cdiv(m, rows) + 1) / 2); };
+  const int bn = halves && triangle(256) >= kSms / 2 ? 256 : triangle(128) >= kSms ? 128 : 64;
   for (int i = 0; i < p.steps && e == cudaSuccess; ++i) {
     const float* const c = p.coefficients + 3 * i;
     const Growth g = grow(most, c[0], c[1], c[2]);
     const double scale_s = scale_for(most * most), scale_p = scale_for(std::max(g.factor, 1e-3));
     const double next = std::max(g.value, 1e-3), scale_next = scale_for(next);
     const bool last = i + 1 == p.steps;
+    const double scale_to = last ? (double)p.scale : scale_next;
     const Image &x = at.x[i & 1], &y = at.x[(i + 1) & 1];
     const auto product = [&](auto tag, OrthogonalArgs& a) {
       using J = typename decltype(tag)::Type;
@@ -868,24 +927,31 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
       a.batch = p.batch;
       const long long items = J::tiles(a.rows, a.cols) * p.batch;
       if (items > INT_MAX) return cudaErrorInvalidValue;
-      return launch<J>(a, (unsigned)std::min<long long>(kSms, items), room);
+      return launch<J>(a, (unsigned)(J::kPair ? std::min<long long>(kSms, 2 * items) : std::min<long long>(kSms, items)), room);
     };
     OrthogonalArgs gram{}, poly{}, move{};
     gram.rows = gram.cols = m;
     gram.k = tall ? p.rows : p.cols;
     gram.factor = (float)(scale_s / (scale * scale));
     gram.to = at.s;
+    gram.to_diagonals = at.s_diagonals;
     poly.rows = poly.cols = poly.k = m;
     poly.factor = (float)(c[2] * scale_p / (scale_s * scale_s));
-    poly.diagonal = (float)(c[0] * scale_p);
+    poly.diagonal = (float)(halves ? c[0] : c[0] * scale_p);
+    poly.unscale = (float)(1.0 / scale_p);
     poly.linear = (float)(c[1] * scale_p / scale_s);
     poly.s = at.s;
     poly.to = at.p;
+    poly.diagonals = at.s_diagonals;
+    poly.to_diagonals = at.p_diagonals;
     move.rows = p.rows;
     move.cols = p.cols;
     move.k = m;
-    move.factor = (float)(last ? p.scale / (scale_p * scale) : scale_next / (scale_p * scale));
+    move.factor = (float)(scale_to / (scale_p * scale));
+    move.linear = (float)(scale_to / scale);
+    move.s = x;
     move.to = y;
+    move.diagonals = at.p_diagonals;
     if (last) {
       move.out = p.out;
       move.out_type = p.out_type;
@@ -893,20 +959,26 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
       move.stride_o = p.stride_o;
       move.vec_o = even(p.out, p.ldo, size_of(p.out_type)) && (p.batch == 1 || p.stride_o * size_of(p.out_type) % 16 == 0);
     }
-    const auto step = [&](auto width) {
-      constexpr int BN = decltype(width)::value;
-      const bool maps = map(&poly.a, at.s, m, kBM) && map(&poly.b, at.s, m, BN) &&
-                        (tall ? map(&gram.a, x, p.cols, kBK) && map(&gram.b, x, p.cols, kBK) && map(&move.a, x, p.cols, kBM) && map(&move.b, at.p, m, BN)
-                              : map(&gram.a, x, p.cols, kBM) && map(&gram.b, x, p.cols, BN) && map(&move.a, at.p, m, kBM) && map(&move.b, x, p.cols, kBK));
+    const auto step = [&](auto parts, auto width) {
+      constexpr int PARTS = decltype(parts)::value, BN = decltype(width)::value;
+      constexpr bool PAIR = BN == 256;
+      constexpr int kRows = PAIR ? kBM : BN;   // of B that one block loads
+      const bool maps = map(&poly.a, at.s, m, kBM) && map(&poly.b, at.s, m, kRows) &&
+                        (tall ? map(&gram.a, x, p.cols, kBK) && map(&gram.b, x, p.cols, kBK) && map(&move.a, x, p.cols, kBM) && map(&move.b, at.p, m, kRows)
+                              : map(&gram.a, x, p.cols, kBM) && map(&gram.b, x, p.cols, kRows) && map(&move.a, at.p, m, kBM) && map(&move.b, x, p.cols, kBK));
       if (!maps) return cudaErrorNotSupported;
-      cudaError_t q = tall ? product(Tag<OrthogonalJob<kGram, BN, true, true>>(), gram) : product(Tag<OrthogonalJob<kGram, BN, false, false>>(), gram);
-      if (q == cudaSuccess) q = product(Tag<OrthogonalJob<kPolynomial, BN, false, false>>(), poly);
-      if (q == cudaSuccess) q = tall ? product(Tag<OrthogonalJob<kMove, BN, false, false>>(), move) : product(Tag<OrthogonalJob<kMove, BN, false, true>>(), move);
+      cudaError_t q = tall ? product(Tag<OrthogonalJob<kGram, PARTS, BN, true, true, PAIR>>(), gram) : product(Tag<OrthogonalJob<kGram, PARTS, BN, false, false, PAIR>>(), gram);
+      if (q == cudaSuccess) q = product(Tag<OrthogonalJob<kPolynomial, PARTS, BN, false, false, PAIR>>(), poly);
+      if (q == cudaSuccess) q = tall ? product(Tag<OrthogonalJob<kMove, PARTS, BN, false, false, PAIR>>(), move) : product(Tag<OrthogonalJob<kMove, PARTS, BN, false, true, PAIR>>(), move);
       return q;
     };
-    // narrower tiles where the wider ones would leave SMs without any
-    const long long blocks = cdiv(m, 128);
-    e = p.batch * blocks * (blocks + 1) / 2 >= kSms ? step(std::integral_constant<int, 128>()) : step(std::integral_constant<int, 64>());
+    const auto wide = [&](auto parts) {
+      if (bn == 64) return step(parts, std::integral_constant<int, 64>());
+      if constexpr (decltype(parts)::value == 1)
+        if (bn == 256) return step(parts, std::integral_constant<int, 256>());
+      return step(parts, std::integral_constant<int, 128>());
+    };
+    e = halves ? wide(std::integral_constant<int, 1>()) : wide(std::integral_constant<int, 2>());
     most = next;
     scale = scale_next;
   }

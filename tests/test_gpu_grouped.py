@@ -390,7 +390,9 @@ def ortho_tolerance(g, coefficients, dtype, eps=1e-7):
     """Bound of ||error|| / ||X||.  A step's products are held to u = 2^-19 of their terms (sums of at most 256 products cut toward zero 16 times
     at 2^-23, and added; pairs hold the operands to 2^-22).  These errors have no direction of their own: they spread evenly over the singular
     directions.  An error along direction i is multiplied by |a + 3 b s_i^2 + 5 c s_i^4| in a step, the derivative of s (a + b s^2 + c s^4); parts that
-    mix two directions by the divided difference of that map, which lies between derivatives of its interval.  Factor 2 for these."""
+    mix two directions by the divided difference of that map, which lies between derivatives of its interval.  Factor 2 for these.
+    bf16 results come from products of halves with the diagonals apart: 2^-12 at most of every element off the diagonals, which is 0.5 to 1.3e-3 of the result
+    and has its place between the rounding of a result, 1.7e-3 in the mean (a uniform error of half a step, over sqrt(3)), and eps / 2."""
     import torch
     x = newton_schulz(g, [], eps, 1.0)
     s = torch.linalg.svdvals(x).reshape(-1)
@@ -416,6 +418,33 @@ def test_orthogonalise(h, kind, batch, rows, cols):
             want = newton_schulz(g, coefficients, 1e-7, 0.2)
             rel = float((x.double() - want).norm() / want.norm())
             assert rel < ortho_tolerance(g, coefficients, x.dtype), (out, coefficients, rel)
+
+
+@pytest.mark.parametrize("kind", NAMES)
+@pytest.mark.parametrize("batch, rows, cols", [(16, 600, 700), (16, 712, 600), (10, 600, 640), (10, 640, 602), (1, 1500, 1400)])
+def test_orthogonalise_larger_ones(h, kind, batch, rows, cols):
+    """Enough tiles for the wider ones, in both orientations."""
+    import torch
+    g = gradient(batch, rows, cols, kind, seed=rows)
+    x = torch.empty_like(g)
+    h.orthogonalise(g.data_ptr(), x.data_ptr(), batch, rows, cols, [MUON] * 5, scale=0.2, type=code(kind))
+    want = newton_schulz(g, [MUON] * 5, 1e-7, 0.2)
+    for i in range(batch):
+        rel = float((x[i].double() - want[i]).norm() / want[i].norm())
+        assert rel < ortho_tolerance(g[i:i + 1], [MUON] * 5, x.dtype), (i, rel)
+
+
+def test_orthogonalise_of_spread_singular_values(h):
+    """A few strong directions above a weak floor, which the steps lift most: half of a bf16 result's tolerance is left for its rounding, 1.7e-3 in the mean."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for m, n in ((300, 700), (640, 200)):
+        g = torch.randn(1, m, 20, generator=gen, device="cuda") @ torch.randn(1, 20, n, generator=gen, device="cuda")
+        g = (g + 1e-3 * torch.randn(1, m, n, generator=gen, device="cuda")).bfloat16()
+        x = torch.empty_like(g)
+        h.orthogonalise(g.data_ptr(), x.data_ptr(), 1, m, n, [MUON] * 5, type=binding.BF16)
+        want = newton_schulz(g, [MUON] * 5, 1e-7, 1.0)
+        assert float((x.double() - want).norm() / want.norm()) < torch.finfo(x.dtype).eps / 2
 
 
 @pytest.mark.parametrize("kind", NAMES)
