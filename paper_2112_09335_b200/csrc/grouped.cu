@@ -80,7 +80,7 @@ template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA, bool PAIR =
 struct ProductJob {
   using T = T_;
   using Args = ProductArgs;
-  static constexpr int kParts = PARTS, kBN = BN, kSegment = 4;
+  static constexpr int kParts = PARTS, kBN = BN;
   static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kMeets = false, kPair = PAIR;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM;
   struct Item {
@@ -92,6 +92,7 @@ struct ProductJob {
   __device__ __forceinline__ ProductJob(const Args& args, uint8_t* tables, int rank_)
       : a(args), groups(tables, args.p.groups), tiles_n((args.p.n + BN - 1) / BN), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return PARTS > 1 || a.p.type == kBf16; }
+  __device__ __forceinline__ int segment() const { return a.p.out_type == kF32 ? 4 : 16; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {
     for (int g = threadIdx.x; g < groups.count; g += blockDim.x) {
@@ -184,7 +185,7 @@ struct ProductTnJob {
   using T = T_;
   using Args = ProductTnArgs;
   using Size = unsigned long long;
-  static constexpr int kParts = PARTS, kBN = BN, kSegment = 4;
+  static constexpr int kParts = PARTS, kBN = BN;
   static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kMeets = true, kPair = PAIR;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kRanks = PAIR ? 2 : 1;
   struct Item {
@@ -207,6 +208,7 @@ struct ProductTnJob {
         last(reinterpret_cast<int*>(tables) + 4 * kMaxGroups), shares(reinterpret_cast<Size*>(tables) + 2 * kMaxGroups + 2), count(args.p.groups), tiles_n((args.p.nb + BN - 1) / BN),
         tiles(tiles_n * ((args.p.ka + kTileRows - 1) / kTileRows)), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return PARTS > 1 || a.p.type == kBf16; }
+  __device__ __forceinline__ int segment() const { return a.p.out_type == kF32 ? 4 : 16; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   // Chunks of a tile of group g; a group without rows has one, which writes zeros.
   __device__ __forceinline__ unsigned chunks_of(int g) const { return (unsigned)max(1, (end[g] - begin[g] + kBK - 1) / kBK); }
@@ -398,20 +400,40 @@ struct Image {
   __device__ __forceinline__ __half* matrix(int b) const { return at + (long long)b * rows * ld; }
 };
 
-constexpr int kNormBlocks = 64;   // partial sums of a norm, at most
+constexpr int kNormBlocks = 256;   // partial sums of a norm, at most
 
-// Partial sums of squares of every matrix; in fp64: squares of fp32 numbers leave the range of fp32.
+// Eight elements of a row, those from `valid` on zero.
 template <typename T>
-__global__ void __launch_bounds__(256) k_norm(const Orthogonal p, double* __restrict__ partial) {
+__device__ __forceinline__ void load8(const T* at, int valid, bool vec, float (&v)[8]) {
+  if (vec && valid >= 8) {
+    uint4 w[sizeof(T) / 2];
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) w[k] = *(reinterpret_cast<const uint4*>(at) + k);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = to_float(reinterpret_cast<const T*>(w)[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = k < valid ? to_float(at[k]) : 0.f;
+  }
+}
+
+// Partial sums of squares of every matrix; in fp64: squares of fp32 numbers leave the range of fp32.  (One load a thread and 64 blocks took 520 us
+// of 4096 x 4096 halves, eight elements a load and as many blocks as there is work for WITH.)
+template <typename T>
+__global__ void __launch_bounds__(256) k_norm(const Orthogonal p, bool vec, double* __restrict__ partial) {
   gtc::enter_kernel();
   __shared__ double s_sum[8];
   const T* const g = static_cast<const T*>(p.g) + (long long)blockIdx.y * p.stride_g;
-  const unsigned cols = p.cols, count = (unsigned)p.rows * cols;
+  const unsigned units = (p.cols + 7) / 8, count = (unsigned)p.rows * units;
   double sum = 0.0;
   for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += gridDim.x * 256) {
-    const unsigned row = e / cols;
-    const double x = (double)to_float(g[row * p.ldg + (e - row * cols)]);
-    sum = fma(x, x, sum);
+    const unsigned row = e / units, col = (e - row * units) * 8;
+    float v[8];
+    load8(g + row * p.ldg + col, p.cols - (int)col, vec, v);
+    double part[2] = {0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) part[k & 1] = fma((double)v[k], (double)v[k], part[k & 1]);
+    sum += part[0] + part[1];
   }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -425,26 +447,27 @@ __global__ void __launch_bounds__(256) k_norm(const Orthogonal p, double* __rest
 
 // X_0 = G / (||G|| + eps), to its image under `scale`; with no steps to take, `scale` times it, to the result.  A thread has eight elements of a row.
 template <typename T, typename O>
-__global__ void __launch_bounds__(256) k_start(const Orthogonal p, const double* __restrict__ partial, int partials, const Image x, float scale) {
+__global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, const double* __restrict__ partial, int partials, const Image x, float scale) {
   gtc::enter_kernel();
-  __shared__ double s_inverse;
-  if (threadIdx.x == 0) {
-    double sum = 0.0;
-    for (int k = 0; k < partials; ++k) sum += partial[blockIdx.y * kNormBlocks + k];
-    const double norm = sqrt(sum) + (double)p.eps;
-    // a zero matrix stays zero, one that is not finite becomes NaN
-    s_inverse = !(norm > 0.0) ? (sum == 0.0 ? 0.0 : nan("")) : norm < INFINITY ? 1.0 / norm : nan("");
-  }
+  __shared__ double s_sum[8];
+  double sum = (int)threadIdx.x < partials ? partial[blockIdx.y * kNormBlocks + threadIdx.x] : 0.0;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
   __syncthreads();
-  const double inverse = s_inverse;
+  sum = 0.0;
+  for (int w = 0; w < 8; ++w) sum += s_sum[w];
+  const double norm = sqrt(sum) + (double)p.eps;
+  // a zero matrix stays zero, one that is not finite becomes NaN
+  const double inverse = !(norm > 0.0) ? (sum == 0.0 ? 0.0 : nan("")) : norm < INFINITY ? 1.0 / norm : nan("");
   const T* const g = static_cast<const T*>(p.g) + (long long)blockIdx.y * p.stride_g;
   const unsigned units = x.ld / 8, count = (unsigned)p.rows * units;
   for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += gridDim.x * 256) {
     const unsigned row = e / units, col = (e - row * units) * 8;
-    const T* const src = g + row * p.ldg + col;
     float v[8];
+    load8(g + row * p.ldg + col, p.cols - (int)col, vec, v);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (int)col + k < p.cols ? (float)((double)to_float(src[k]) * inverse) * scale : 0.f;
+    for (int k = 0; k < 8; ++k) v[k] = (float)((double)v[k] * inverse) * scale;
     if (x.at != nullptr) {
       uint32_t hi[4], lo[4];
 #pragma unroll
@@ -484,42 +507,10 @@ struct OrthogonalArgs {
   bool vec_o;
 };
 
-// 32 rows x NC columns of halves as the NC rows x 32 columns of the turned matrix at `out`.
-template <int NC>
-__device__ __forceinline__ void store_turned(const float (&acc)[NC], uint8_t* buf, __half* out, long long ld, int rows_left, int cols_left) {
-  const int lane = threadIdx.x & 31, q = lane & 3;
-#pragma unroll
-  for (int c0 = 0; c0 < NC; c0 += 32) {
-    if (c0 < cols_left) {
-#pragma unroll
-      for (int c = 0; c < 32; ++c)
-        *reinterpret_cast<__half*>(buf + c * 64 + (((lane >> 3) ^ ((c >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2half_rn(acc[c0 + c]);
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = 8 * i + (lane >> 2), some = rows_left - 8 * q;
-        const uint4 v = *reinterpret_cast<const uint4*>(buf + c * 64 + ((q ^ ((c >> 1) & 3)) << 4));
-        __half* const at = out + (c0 + c) * ld + 8 * q;
-        if (c0 + c < cols_left && some > 0) {
-          if (some >= 8) {
-            *reinterpret_cast<uint4*>(at) = v;
-          } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e < some) reinterpret_cast<unsigned short*>(at)[e] = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
-          }
-        }
-      }
-      __syncwarp();
-    }
-  }
-}
-
 template <Stage STAGE, int PARTS, int BN, bool A_MN, bool B_MN, bool PAIR>
 struct OrthogonalJob {
   using Args = OrthogonalArgs;
-  static constexpr int kParts = PARTS, kBN = BN, kSegment = PARTS == 1 ? 4 : 1;   // pairs are for results that show where sums are cut
+  static constexpr int kParts = PARTS, kBN = BN;
   static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kBCols = PAIR ? BN / 2 : BN;
   struct Item {
@@ -530,6 +521,8 @@ struct OrthogonalJob {
   int rank;
   __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int rank_) : a(args), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return false; }
+  // pairs are for results that show where sums are cut (1000 x 767 in fp32: 4.7e-6 off with segments of 4 chunks, 1.4e-6 with one)
+  __device__ __forceinline__ int segment() const { return PARTS == 1 ? 16 : 1; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {}
   // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kTileRows / BN (i + 1)
@@ -590,85 +583,147 @@ struct OrthogonalJob {
       }
     }
   }
-  // f(column, hi, lo) for the elements of a row of an image, eight at a time (rows are padded to that); LO: whether lo is there.
-  template <int NC, bool LO, typename F>
-  __device__ __forceinline__ static void for_row(const Image& im, const __half* at, int cols_left, const F& f) {
+  // 32 elements of this lane's row of a part of an image, from column c0 on, as 16 words: whole sectors come in and are handed out through the buffer.
+  __device__ __forceinline__ static void take(const RowStore& through, const __half* at, int ld, int c0, int rows_left, int cols_left, uint32_t (&w)[16]) {
+    const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
 #pragma unroll
-    for (int c0 = 0; c0 < NC; c0 += 8) {
-      asm volatile("" ::: "memory");   // one unit at a time: all loads at once do not fit the registers
-      if (c0 < cols_left) {
-        const uint4 hi = *reinterpret_cast<const uint4*>(at + c0), lo = LO ? *reinterpret_cast<const uint4*>(at + im.part + c0) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + r0;
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (r < rows_left && c0 + 8 * q < cols_left) v = *reinterpret_cast<const uint4*>(at + (long long)r * ld + c0 + 8 * q);
+      *reinterpret_cast<uint4*>(through.unit(r, q)) = v;
+    }
+    __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
-          f(c0 + 2 * e, LO ? fmaf(y.x, 0x1p-11f, x.x) : x.x);
-          f(c0 + 2 * e + 1, LO ? fmaf(y.y, 0x1p-11f, x.y) : x.y);
+    for (int u = 0; u < 4; ++u) {
+      const uint4 v = *reinterpret_cast<const uint4*>(through.unit(lane, u));
+      w[4 * u] = v.x; w[4 * u + 1] = v.y; w[4 * u + 2] = v.z; w[4 * u + 3] = v.w;
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ static float2 floats(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+  // 32 rows x 32 columns of halves, a row a lane, as 32 rows x 32 columns of the turned matrix at `out`.
+  __device__ __forceinline__ static void put_turned(const RowStore& through, const uint32_t (&w)[16], __half* out, long long ld, int rows_left, int cols_left) {
+    const int lane = threadIdx.x & 31, q = lane & 3;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      *reinterpret_cast<unsigned short*>(through.unit(c, lane >> 3) + (lane & 7) * 2) = (unsigned short)(w[c >> 1] >> (16 * (c & 1)));
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 8 * i + (lane >> 2), some = rows_left - 8 * q;
+      __half* const at = out + c * ld + 8 * q;
+      if (c < cols_left && some > 0) {
+        const uint4 v = *reinterpret_cast<const uint4*>(through.unit(c, q));
+        if (some >= 8) {
+          *reinterpret_cast<uint4*>(at) = v;
+        } else {
+          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < some) reinterpret_cast<unsigned short*>(at)[e] = (unsigned short)(x[e >> 1] >> (16 * (e & 1)));
         }
       }
     }
+    __syncwarp();
   }
+  // 32 columns at a time from sums to what is stored of them: few registers beside the sums
   template <int NC>
   __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], uint8_t* buf, int warp) const {
-    const int row0 = it.row0 + (warp & 3) * 32, col0 = it.col0 + (warp >> 2) * NC, row = row0 + (threadIdx.x & 31);
+    const int row0 = it.row0 + (warp & 3) * 32, col0 = it.col0 + (warp >> 2) * NC, lane = threadIdx.x & 31, row = row0 + lane;
     const int rows_left = a.rows - row0, cols_left = a.cols - col0;
     if (rows_left <= 0 || cols_left <= 0) return;
-    const int own = min(row, a.rows - 1);   // a row that exists
     const bool diagonal = kSymmetric && row0 < col0 + NC && col0 < row0 + 32;   // whether the warp holds some of it
+    // 1 part: the diagonal entry of this lane's row, and those of the columns, NC / 32 a lane
+    constexpr bool kTall = STAGE == kMove && !B_MN;
+    const float* const d = PARTS == 1 && STAGE != kGram ? a.diagonals + (long long)it.matrix * (kTall ? a.cols : a.rows) : nullptr;
+    float mine = 0.f, theirs[NC / 32] = {};
+    if (PARTS == 1 && STAGE != kGram) {
+      if (!kTall) mine = d[min(row, a.rows - 1)];
+      if (STAGE == kPolynomial || kTall)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] *= a.factor;
-    if constexpr (STAGE == kPolynomial) {
-      const __half* const s = a.s.matrix(it.matrix) + (long long)own * a.s.ld + col0;
-      if constexpr (PARTS == 2) {
-        for_row<NC, true>(a.s, s, cols_left, [&](int c, float x) { acc[c] = fmaf(a.linear, x, acc[c]); });
-        if (diagonal) {
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-            if (row == col0 + c) acc[c] += a.diagonal;
-        }
-      } else {
-        const float* const d = a.diagonals + (long long)it.matrix * a.rows;
-        const float mine = d[own];
-        // acc is c O O under the scale of P: with the diagonals of S, b O + c (O O + (D_i + D_j) O); on the diagonal b D + c (O O + D D)
-        for_row<NC, false>(a.s, s, cols_left, [&](int c, float x) { acc[c] = fmaf(x, fmaf(a.factor, mine + d[min(col0 + c, a.cols - 1)], a.linear), acc[c]); });
-        if (diagonal) {
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-            if (row == col0 + c) acc[c] = fmaf(mine, fmaf(a.factor, mine, a.linear), acc[c]);
-        }
-      }
+        for (int k = 0; k < NC / 32; ++k) theirs[k] = d[min(col0 + 32 * k + lane, a.cols - 1)];
     }
-    if (PARTS == 1 && diagonal) {
-      float* const to = a.to_diagonals + (long long)it.matrix * a.rows;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (row == col0 + c) {
-          if (row < a.rows) to[row] = STAGE == kPolynomial ? fmaf(acc[c], a.unscale, a.diagonal) : acc[c];
-          acc[c] = 0.f;
-        }
-    }
-    if constexpr (PARTS == 1 && STAGE == kMove) {
-      constexpr bool kTall = !B_MN;
-      const float* const d = a.diagonals + (long long)it.matrix * (kTall ? a.cols : a.rows);
-      const float by_row = kTall ? 0.f : d[own] * a.linear;
-      const __half* const x = a.s.matrix(it.matrix) + (long long)own * a.s.ld + col0;
-      for_row<NC, true>(a.s, x, cols_left, [&](int c, float v) { acc[c] = fmaf(v, kTall ? d[min(col0 + c, a.cols - 1)] * a.linear : by_row, acc[c]); });
-    }
-    if (STAGE == kMove && a.out != nullptr) {
-      const long long at = (long long)it.matrix * a.stride_o + row0 * a.ldo + col0;
-      void* const out = a.out_type == kF32 ? (void*)(static_cast<float*>(a.out) + at) : (void*)(static_cast<unsigned short*>(a.out) + at);
-      store_rows<NC>(acc, buf, out, a.ldo, a.out_type, a.vec_o, rows_left, cols_left);
-      return;
-    }
+    const bool out = STAGE == kMove && a.out != nullptr;
+    const int out_size = a.out_type == kF32 ? 4 : 2;
     __half* const to = a.to.matrix(it.matrix);
     // images have room up to their leading dimension, and whole units there
-    store_rows<NC>(acc, buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
-    if (it.turn) store_turned<NC>(acc, buf, to + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
-    if constexpr (PARTS == 2 || STAGE == kMove) {
+    const RowStore hi_to = out ? RowStore(buf, static_cast<uint8_t*>(a.out) + ((long long)it.matrix * a.stride_o + row0 * a.ldo + col0) * out_size, a.ldo, out_size, a.vec_o, rows_left, cols_left)
+                               : RowStore(buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, 2, true, rows_left, a.to.ld - col0);
+    const __half* const from = STAGE == kGram ? nullptr : a.s.matrix(it.matrix) + (long long)row0 * a.s.ld + col0;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) acc[c] = (acc[c] - __half2float(__float2half_rn(acc[c]))) * 0x1p11f;
-      store_rows<NC>(acc, buf, to + a.to.part + (long long)row0 * a.to.ld + col0, a.to.ld, kF16, true, rows_left, a.to.ld - col0);
-      if (it.turn) store_turned<NC>(acc, buf, to + a.to.part + (long long)col0 * a.to.ld + row0, a.to.ld, rows_left, cols_left);
+    for (int c0 = 0; c0 < NC; c0 += 32) {
+      if (c0 < cols_left) {
+        float x[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] = acc[c0 + c] * a.factor;
+        if constexpr (STAGE == kPolynomial || (STAGE == kMove && PARTS == 1)) {
+          uint32_t h[16];
+          take(hi_to, from, a.s.ld, c0, rows_left, a.s.ld - col0, h);
+          // of S b, with its diagonals apart b + c (D_i + D_j); of X the diagonal of P and a
+          const auto weight = [&](int c) {
+            if (STAGE == kPolynomial) return PARTS == 1 ? fmaf(a.factor, mine + __shfl_sync(0xffffffffu, theirs[c0 / 32], c), a.linear) : a.linear;
+            return (kTall ? __shfl_sync(0xffffffffu, theirs[c0 / 32], c) : mine) * a.linear;
+          };
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float2 v = floats(h[e]);
+            x[2 * e] = fmaf(weight(2 * e), v.x, x[2 * e]);
+            x[2 * e + 1] = fmaf(weight(2 * e + 1), v.y, x[2 * e + 1]);
+          }
+          if constexpr (PARTS == 2 || STAGE == kMove) {
+            take(hi_to, from + a.s.part, a.s.ld, c0, rows_left, a.s.ld - col0, h);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float2 v = floats(h[e]);
+              x[2 * e] = fmaf(weight(2 * e) * 0x1p-11f, v.x, x[2 * e]);
+              x[2 * e + 1] = fmaf(weight(2 * e + 1) * 0x1p-11f, v.y, x[2 * e + 1]);
+            }
+          }
+        }
+        if (diagonal) {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            if (row == col0 + c0 + c) {
+              if constexpr (PARTS == 2) {
+                if (STAGE == kPolynomial) x[c] += a.diagonal;
+              } else {   // the image has none: O O alone is in x, b D + c D D is added
+                if (STAGE == kPolynomial) x[c] = fmaf(fmaf(fmaf(a.factor, mine, a.linear), mine, x[c]), a.unscale, a.diagonal);
+                if (row < a.rows) a.to_diagonals[(long long)it.matrix * a.rows + row] = x[c];
+                x[c] = 0.f;
+              }
+            }
+          }
+        }
+        if (out && a.out_type == kF32) {
+#pragma unroll
+          for (int half = 0; half < 32; half += 16)
+            if (c0 + half < cols_left)
+              hi_to.put(c0 + half, words(x[half], x[half + 1], x[half + 2], x[half + 3]), words(x[half + 4], x[half + 5], x[half + 6], x[half + 7]),
+                        words(x[half + 8], x[half + 9], x[half + 10], x[half + 11]), words(x[half + 12], x[half + 13], x[half + 14], x[half + 15]));
+        } else {
+          const int type = out ? a.out_type : (int)kF16;
+          uint32_t h[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) h[e] = pack(type, x[2 * e], x[2 * e + 1]);
+          hi_to.put(c0, make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7]), make_uint4(h[8], h[9], h[10], h[11]), make_uint4(h[12], h[13], h[14], h[15]));
+          if (!out) {
+            __half* const turned = to + (long long)(col0 + c0) * a.to.ld + row0;
+            if (it.turn) put_turned(hi_to, h, turned, a.to.ld, rows_left, cols_left - c0);
+            if constexpr (PARTS == 2 || STAGE == kMove) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float2 v = floats(h[e]);
+                h[e] = pack(kF16, (x[2 * e] - v.x) * 0x1p11f, (x[2 * e + 1] - v.y) * 0x1p11f);
+              }
+              RowStore lo_to = hi_to;
+              lo_to.out += 2 * a.to.part;
+              lo_to.put(c0, make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7]), make_uint4(h[8], h[9], h[10], h[11]), make_uint4(h[12], h[13], h[14], h[15]));
+              if (it.turn) put_turned(hi_to, h, turned + a.to.part, a.to.ld, rows_left, cols_left - c0);
+            }
+          }
+        }
+      }
     }
   }
 };
@@ -761,16 +816,19 @@ struct Tag {
 
 }  // namespace
 
-// Tiles of a weight gradient: 256 x 256 by pairs of blocks where both widths fill them, else 128 rows by what the columns need.
+// Tiles of a weight gradient: 256 x 256 by pairs of blocks where both widths fill them, else 128 rows by what the columns need and the registers of a
+// block that loads through them allow.
 struct TnPlan {
   int bn, ranks;     // ranks: blocks of a tile
+  bool tma;
   unsigned grid;
 };
 TnPlan plan(const ProductTn& p) {
   const bool wide = p.type != kF32;
   const int size = size_of(p.type);
-  const bool pair = wide && p.rows > 0 && fits_pairs(p.ka) && fits_pairs(p.nb) && even(p.x, p.ldx, size) && even(p.y, p.ldy, size) && gcn_admm_host::encode_tiled() != nullptr;
-  TnPlan t{p.nb <= 64 ? 64 : p.nb <= 128 || !wide ? 128 : 256, pair ? 2 : 1, kSms};
+  const bool tma = wide && p.rows > 0 && even(p.x, p.ldx, size) && even(p.y, p.ldy, size) && gcn_admm_host::encode_tiled() != nullptr;
+  const bool pair = tma && fits_pairs(p.ka) && fits_pairs(p.nb);
+  TnPlan t{p.nb <= 64 ? 64 : p.nb <= 128 || !tma ? 128 : 256, pair ? 2 : 1, tma, kSms};
   // no more than there is work for: chunks at most, wherever the groups begin, and not fewer than tiles
   const long long tiles = cdiv(p.ka, t.ranks * kBM) * cdiv(p.nb, t.bn), chunks = tiles * (cdiv(p.rows, kBK) + p.groups);
   t.grid = (unsigned)std::min<long long>(kSms, t.ranks * std::max<long long>(1, chunks / kLeastChunks));
@@ -878,15 +936,17 @@ cudaError_t enqueue(const ProductTn& p, const Room& room) {
   const auto width = [&](const auto& f) {
     return t.bn == 256 ? f(std::integral_constant<int, 256>()) : t.bn == 128 ? f(std::integral_constant<int, 128>()) : f(std::integral_constant<int, 64>());
   };
-  if (p.type == kF32)
-    return width([&](auto w) {
-      if constexpr (decltype(w)::value == 256) return cudaErrorNotSupported;
-      else if (a.vec_x && a.vec_y && p.ka % 4 == 0 && p.nb % 4 == 0) return launch<ProductTnJob<float, 3, decltype(w)::value, false, false, true>>(a, grid, room);
-      else return launch<ProductTnJob<float, 3, decltype(w)::value, false>>(a, grid, room);
-    });
-  if (p.rows > 0 && a.vec_x && a.vec_y && make_map(&a.a, p.type, p.x, p.ka, p.rows, p.ldx, 1, 0, kBK) && make_map(&a.b, p.type, p.y, p.nb, p.rows, p.ldy, 1, 0, kBK))
+  if (t.tma) {
+    if (!make_map(&a.a, p.type, p.x, p.ka, p.rows, p.ldx, 1, 0, kBK) || !make_map(&a.b, p.type, p.y, p.nb, p.rows, p.ldy, 1, 0, kBK)) return cudaErrorNotSupported;
     return width([&](auto w) { return launch<ProductTnJob<unsigned short, 1, decltype(w)::value, true>>(a, grid, room); });
-  return width([&](auto w) { return launch<ProductTnJob<unsigned short, 1, decltype(w)::value, false>>(a, grid, room); });
+  }
+  return width([&](auto w) {
+    constexpr int BN = decltype(w)::value;
+    if constexpr (BN == 256) return cudaErrorNotSupported;
+    else if (p.type != kF32) return launch<ProductTnJob<unsigned short, 1, BN, false>>(a, grid, room);
+    else if (a.vec_x && a.vec_y && p.ka % 4 == 0 && p.nb % 4 == 0) return launch<ProductTnJob<float, 3, BN, false, false, true>>(a, grid, room);
+    else return launch<ProductTnJob<float, 3, BN, false>>(a, grid, room);
+  });
 }
 
 cudaError_t enqueue(const Orthogonal& p, const Room& room) {
@@ -898,12 +958,13 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
   const auto scale_for = [](double most) { return std::ldexp(1.0, 14 - std::ilogb(most)); };
   double most = 1.0, scale = p.steps > 0 ? scale_for(most) : (double)p.scale;
   const long long elements = (long long)p.rows * p.cols;
-  const int partials = (int)std::min<long long>(kNormBlocks, cdiv(elements, 2048));
+  const int partials = (int)std::min<long long>(kNormBlocks, cdiv(elements, 4096));
+  const bool vec = even(p.g, p.ldg, size_of(p.type)) && (p.batch == 1 || p.stride_g * size_of(p.type) % 16 == 0);
   cudaError_t e = cudaSuccess;
-  with_type(p.type, [&](auto in) { e = launch_plain(k_norm<decltype(in)>, dim3((unsigned)partials, (unsigned)p.batch), room, p, at.partial); });
+  with_type(p.type, [&](auto in) { e = launch_plain(k_norm<decltype(in)>, dim3((unsigned)partials, (unsigned)p.batch), room, p, vec, at.partial); });
   if (e != cudaSuccess) return e;
   with_types(p.type, p.out_type, [&](auto in, auto out) {
-    e = launch_plain(k_start<decltype(in), decltype(out)>, dim3((unsigned)std::min<long long>(1024, cdiv(elements, 2048)), (unsigned)p.batch), room, p, at.partial, partials,
+    e = launch_plain(k_start<decltype(in), decltype(out)>, dim3((unsigned)std::min<long long>(1024, cdiv(elements, 2048)), (unsigned)p.batch), room, p, vec, at.partial, partials,
                      p.steps > 0 ? at.x[0] : none, (float)scale);
   });
   const bool halves = p.out_type == kBf16;   // one part is enough

@@ -21,7 +21,7 @@
 //       what is left out is below 2^-21 of |x||y|, 2^-24 in the mean.
 // The main product and the corrections have accumulators of their own.  The tensor core cuts an accumulator toward zero at every
 // instruction; an error that grows with the length of the reduction is kept out by taking the accumulator into registers after
-// every segment of 256 steps, where segments are added in fp32 (rounded to nearest).  Two accumulators alternate, so that instructions of a segment run
+// every segment of 256 steps or fewer (1024 where a result of 16 bits would not show it), where segments are added in fp32, rounded to nearest.  Two accumulators alternate, so that instructions of a segment run
 // beside the reading of the one before it.
 #pragma once
 #include <cuda_bf16.h>
@@ -163,39 +163,50 @@ __device__ __forceinline__ uint32_t pack(int type, float x, float y) {
   const __half2 b = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&b);
 }
-template <int NC>
-__device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf, void* out, long long ld, int out_type, bool vec, int rows_left, int cols_left) {
-  const int lane = threadIdx.x & 31, q = lane & 3;
-  uint8_t* const mine = buf + lane * 64;
-  const int turn = (lane >> 1) & 3;
-  const auto unit = [&](int r, int u) { return buf + r * 64 + ((u ^ ((r >> 1) & 3)) << 4); };
-  const bool wide = out_type == kF32;
-  const int step = wide ? 16 : 32, size = wide ? 4 : 2;   // columns in the buffer at a time
-  const bool whole = vec && rows_left >= 32, quads = vec && (cols_left * size & 15) == 0;
-  // what this lane writes of a row of whole units: unit q of row lane / 4, of that row + 8, ..
-  uint8_t* at = static_cast<uint8_t*>(out) + (lane >> 2) * ld * size + 16 * q;
-  const long long down = 8 * ld * size;
-  const uint8_t* const from = unit(lane >> 2, q);         // rows 8 apart have the same turn: 512 bytes apart
-  const auto leave = [&](int c0) {
+__device__ __forceinline__ uint4 words(float x, float y, float z, float w) {
+  return make_uint4(__float_as_uint(x), __float_as_uint(y), __float_as_uint(z), __float_as_uint(w));
+}
+struct RowStore {
+  uint8_t* buf;
+  uint8_t* out;
+  long long ld;
+  int size, rows_left, cols_left;   // size: bytes of an element
+  bool whole, units;                // all rows there; rows of whole units of 16 bytes
+  __device__ __forceinline__ RowStore(uint8_t* buf_, void* out_, long long ld_, int size_, bool vec, int rows_left_, int cols_left_)
+      : buf(buf_), out(static_cast<uint8_t*>(out_)), ld(ld_), size(size_), rows_left(rows_left_), cols_left(cols_left_), whole(vec && rows_left_ >= 32),
+        units(vec && (cols_left_ * size_ & 15) == 0) {}
+  __device__ __forceinline__ uint8_t* unit(int r, int u) const { return buf + r * 64 + ((u ^ ((r >> 1) & 3)) << 4); }
+  // 64 bytes of this lane's row, from column c0 on.
+  __device__ __forceinline__ void put(int c0, const uint4& w0, const uint4& w1, const uint4& w2, const uint4& w3) const {
+    const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
+    *reinterpret_cast<uint4*>(unit(lane, 0)) = w0;
+    *reinterpret_cast<uint4*>(unit(lane, 1)) = w1;
+    *reinterpret_cast<uint4*>(unit(lane, 2)) = w2;
+    *reinterpret_cast<uint4*>(unit(lane, 3)) = w3;
     __syncwarp();
-    if (whole && cols_left - c0 >= step) {
+    const uint8_t* const from = unit(r0, q);         // rows 8 apart have the same turn: 512 bytes apart
+    if (units) {
+      uint8_t* const at = out + (r0 * ld + c0) * size + 16 * q;
+      const long long down = 8 * ld * size;
+      if (whole && (cols_left - c0) * size >= 64) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
-    } else if (quads) {
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (8 * i + (lane >> 2) < rows_left && c0 * size + 16 * q < cols_left * size) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
-    } else if (wide) {
+        for (int i = 0; i < 4; ++i)
+          if (8 * i + r0 < rows_left && c0 * size + 16 * q < cols_left * size) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
+      }
+    } else if (size == 4) {
       const int c = lane & 15;
       for (int r = lane >> 4; r < min(32, rows_left); r += 2)
-        if (c0 + c < cols_left) static_cast<float*>(out)[r * ld + c0 + c] = reinterpret_cast<const float*>(unit(r, c >> 2))[c & 3];
+        if (c0 + c < cols_left) reinterpret_cast<float*>(out)[r * ld + c0 + c] = reinterpret_cast<const float*>(unit(r, c >> 2))[c & 3];
     } else {
       // word j of a row holds columns 2 j and 2 j + 1, or, where the row starts in the middle of a word, 2 j - 1 and 2 j: then the first and
       // the last column of the step go alone
       const int j = lane & 15, some = cols_left - c0;
       const auto half = [&](int r, int c) { return (uint32_t)reinterpret_cast<const unsigned short*>(unit(r, c >> 3))[c & 7]; };
       for (int r = lane >> 4; r < min(32, rows_left); r += 2) {
-        unsigned short* const row = static_cast<unsigned short*>(out) + r * ld + c0;
+        unsigned short* const row = reinterpret_cast<unsigned short*>(out) + r * ld + c0;
         const int c = 2 * j - (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
         if (c >= 0 && c + 1 < some) *reinterpret_cast<uint32_t*>(row + c) = half(r, c) | half(r, c + 1) << 16;
         else if (c >= 0 && c < some) row[c] = (unsigned short)half(r, c);
@@ -203,29 +214,34 @@ __device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf,
         if (j == 15 && c < 30 && 31 < some) row[31] = (unsigned short)half(r, 31);
       }
     }
-    at += 64;
     __syncwarp();
-  };
-  if (wide) {
+  }
+};
+template <int NC>
+__device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf, void* out, long long ld, int out_type, bool vec, int rows_left, int cols_left) {
+  const RowStore to(buf, out, ld, out_type == kF32 ? 4 : 2, vec, rows_left, cols_left);
+  if (out_type == kF32) {
 #pragma unroll
     for (int c0 = 0; c0 < NC; c0 += 16) {
       if (c0 < cols_left) {
+        uint4 w[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(mine + ((u ^ turn) << 4)) = make_float4(acc[c0 + 4 * u], acc[c0 + 4 * u + 1], acc[c0 + 4 * u + 2], acc[c0 + 4 * u + 3]);
-        leave(c0);
+        for (int u = 0; u < 4; ++u)
+          w[u] = words(acc[c0 + 4 * u], acc[c0 + 4 * u + 1], acc[c0 + 4 * u + 2], acc[c0 + 4 * u + 3]);
+        to.put(c0, w[0], w[1], w[2], w[3]);
       }
     }
   } else {
 #pragma unroll
     for (int c0 = 0; c0 < NC; c0 += 32) {
       if (c0 < cols_left) {
+        uint4 w[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const float* const x = acc + c0 + 8 * u;
-          *reinterpret_cast<uint4*>(mine + ((u ^ turn) << 4)) =
-              make_uint4(pack(out_type, x[0], x[1]), pack(out_type, x[2], x[3]), pack(out_type, x[4], x[5]), pack(out_type, x[6], x[7]));
+          w[u] = make_uint4(pack(out_type, x[0], x[1]), pack(out_type, x[2], x[3]), pack(out_type, x[4], x[5]), pack(out_type, x[6], x[7]));
         }
-        leave(c0);
+        to.put(c0, w[0], w[1], w[2], w[3]);
       }
     }
   }
@@ -282,7 +298,8 @@ struct Raw<unsigned short> {
 };
 
 // The shared loop.  A job J says what the items are, where operand tiles come from and what becomes of a tile's sums:
-//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kPair, kSegment (chunks), kMeets (finish() has barriers of the epilogue warps)
+//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kPair, kMeets (finish() has barriers of the epilogue warps)
+//   segment()                         chunks of a segment, a power of two
 //   J(args, tables, rank)             built by every thread (rank: of the block in its pair); setup(): tables in shared memory, by the whole
 //                                     block, between barriers
 //   J::Walk start(worker, workers)    where this block's (pair's) items begin
@@ -298,7 +315,7 @@ using GeometryOf = Geometry<J::kParts, J::kBN, J::kTma, J::kPair>;
 template <class J>
 __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const __grid_constant__ typename J::Args args) {
   using G = GeometryOf<J>;
-  constexpr int S = G::kStages, BN = J::kBN, PARTS = J::kParts, kSegment = J::kSegment;
+  constexpr int S = G::kStages, BN = J::kBN, PARTS = J::kParts;
   constexpr bool PAIR = J::kPair;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) Bars bars;
@@ -345,6 +362,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
   volatile int* const abortp = &abort_flag;
+  const int segment = job.segment();
   int copies = 0;   // stages this thread has started copies into
   typename J::Item it;
   typename J::Walk walk = job.start(worker, workers);
@@ -450,7 +468,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       while (more) {
         if (!__all_sync(0xffffffffu, gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp))) break;
         uint8_t* const st = smem + (size_t)slot * G::kStage;
-        const bool first = c % kSegment == 0, ends = c + 1 == it.chunks || c % kSegment == kSegment - 1;
+        const bool first = (c & (segment - 1)) == 0, ends = c + 1 == it.chunks || (c & (segment - 1)) == segment - 1;
         const int columns = it.n;
         ++c;
         settle();
@@ -490,7 +508,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
     bool ok = rank == 0;
     while (ok && job.next(walk, it)) {
       for (int c = 0; c < it.chunks; ++c) {
-        const bool first = c % kSegment == 0, last = c + 1 == it.chunks, ends = last || c % kSegment == kSegment - 1;
+        const bool first = (c & (segment - 1)) == 0, last = c + 1 == it.chunks, ends = last || (c & (segment - 1)) == segment - 1;
         const bool clears = J::kAMn && last && it.tail < kBK;
         ok = __all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
                                          gtc::mbar_wait_abortable(full + 8 * slot, parity, abortp));
@@ -519,7 +537,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
 #pragma unroll
       for (int c = 0; c < NC; ++c) acc[c] = 0.f;
       const bool mine = (warp >> 2) * NC < it.n;   // whether any of the warp's columns are asked for
-      for (int c = 0; c < it.chunks; c += kSegment) {
+      for (int c = 0; c < it.chunks; c += segment) {
         ok = __all_sync(0xffffffffu, gtc::mbar_wait_abortable(acc_full + 8 * set, parity, abortp));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
