@@ -3,6 +3,7 @@
 
 #include <atomic>
 #include <climits>
+#include <type_traits>
 
 #include "grouped_mma.cuh"
 #include "tensor_map.hpp"
@@ -150,8 +151,10 @@ struct ProductJob {
       raw.template load<VEC>(w + (long long)k * a.p.ldw + it.col0 + col, k < a.p.k ? it.n - col : 0);
     }
   }
+  using Early = Nothing;
+  __device__ __forceinline__ void early(const Item&, int, Early&) const {}
   template <int NC>
-  __device__ __forceinline__ void finish(const Item& it, const float (&acc)[NC], uint8_t* buf, int warp) const {
+  __device__ __forceinline__ void finish(const Item& it, const float (&acc)[NC], Early&, uint8_t* buf, int warp) const {
     const int row = (warp & 3) * 32, col = (warp >> 2) * NC;
     const long long at = (it.row0 + row) * a.p.ldy + it.col0 + col;
     void* const y = a.p.out_type == kF32 ? (void*)(static_cast<float*>(a.p.y) + at) : (void*)(static_cast<unsigned short*>(a.p.y) + at);
@@ -351,8 +354,10 @@ struct ProductTnJob {
     asm volatile("bar.sync 1, 256;" ::: "memory");
     return all;
   }
+  using Early = Nothing;
+  __device__ __forceinline__ void early(const Item&, int, Early&) const {}
   template <int NC>
-  __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], uint8_t* buf, int warp) const {
+  __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], Early&, uint8_t* buf, int warp) const {
     const int row = it.m0 + (warp & 3) * 32, col = it.col0 + (warp >> 2) * NC;
     if (it.pieces > 1) {
       const int columns = a.p.ka - row > 0 ? a.p.nb - col : 0;   // that come to anything
@@ -522,7 +527,7 @@ struct OrthogonalJob {
   __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int rank_) : a(args), rank(rank_) {}
   __device__ __forceinline__ bool bf16() const { return false; }
   // pairs are for results that show where sums are cut (1000 x 767 in fp32: 4.7e-6 off with segments of 4 chunks, 1.4e-6 with one)
-  __device__ __forceinline__ int segment() const { return PARTS == 1 ? 16 : 1; }
+  __device__ __forceinline__ int segment() const { return PARTS == 1 ? 16 : 2; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {}
   // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kTileRows / BN (i + 1)
@@ -583,16 +588,33 @@ struct OrthogonalJob {
       }
     }
   }
-  // 32 elements of this lane's row of a part of an image, from column c0 on, as 16 words: whole sectors come in and are handed out through the buffer.
-  __device__ __forceinline__ static void take(const RowStore& through, const __half* at, int ld, int c0, int rows_left, int cols_left, uint32_t (&w)[16]) {
+  // 32 rows x 32 columns of an image, from column c0 on, as they lie in memory: whole sectors, eight rows at a time.  On their way while the columns
+  // before are worked on, the first while the tile's products are formed: 16 of 1024 x 2048, this product WAS us where each
+  // was waited for, WITH us so.
+  static constexpr bool kReads = STAGE == kPolynomial || (STAGE == kMove && PARTS == 1);
+  [[maybe_unused]] static constexpr bool kReadsLow = PARTS == 2 ? STAGE == kPolynomial : STAGE == kMove;
+  struct Block {
+    uint4 hi[4], lo[kReadsLow ? 4 : 1];
+  };
+  using Early = std::conditional_t<kReads, Block, Nothing>;
+  __device__ __forceinline__ void fetch(const Item& it, int row0, int col, Block& b) const {
     const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
+    const __half* const at = a.s.matrix(it.matrix) + (long long)(row0 + r0) * a.s.ld + col + 8 * q;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = 8 * i + r0;
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (r < rows_left && c0 + 8 * q < cols_left) v = *reinterpret_cast<const uint4*>(at + (long long)r * ld + c0 + 8 * q);
-      *reinterpret_cast<uint4*>(through.unit(r, q)) = v;
+      const bool there = row0 + 8 * i + r0 < a.s.rows && col + 8 * q < a.s.ld;
+      b.hi[i] = there ? *reinterpret_cast<const uint4*>(at + (long long)8 * i * a.s.ld) : make_uint4(0u, 0u, 0u, 0u);
+      if (kReadsLow) b.lo[i] = there ? *reinterpret_cast<const uint4*>(at + (long long)8 * i * a.s.ld + a.s.part) : make_uint4(0u, 0u, 0u, 0u);
     }
+  }
+  __device__ __forceinline__ void early(const Item& it, int warp, Early& b) const {
+    if constexpr (kReads) fetch(it, it.row0 + (warp & 3) * 32, it.col0 + (warp >> 2) * (BN / 2), b);
+  }
+  // This lane's row of such a block, as 16 words, through the buffer.
+  __device__ __forceinline__ static void hand_out(const RowStore& through, const uint4 (&b)[4], uint32_t (&w)[16]) {
+    const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(through.unit(8 * i + r0, q)) = b[i];
     __syncwarp();
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -629,7 +651,7 @@ struct OrthogonalJob {
   }
   // 32 columns at a time from sums to what is stored of them: few registers beside the sums
   template <int NC>
-  __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], uint8_t* buf, int warp) const {
+  __device__ __forceinline__ void finish(const Item& it, float (&acc)[NC], Early& next, uint8_t* buf, int warp) const {
     const int row0 = it.row0 + (warp & 3) * 32, col0 = it.col0 + (warp >> 2) * NC, lane = threadIdx.x & 31, row = row0 + lane;
     const int rows_left = a.rows - row0, cols_left = a.cols - col0;
     if (rows_left <= 0 || cols_left <= 0) return;
@@ -650,16 +672,17 @@ struct OrthogonalJob {
     // images have room up to their leading dimension, and whole units there
     const RowStore hi_to = out ? RowStore(buf, static_cast<uint8_t*>(a.out) + ((long long)it.matrix * a.stride_o + row0 * a.ldo + col0) * out_size, a.ldo, out_size, a.vec_o, rows_left, cols_left)
                                : RowStore(buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, 2, true, rows_left, a.to.ld - col0);
-    const __half* const from = STAGE == kGram ? nullptr : a.s.matrix(it.matrix) + (long long)row0 * a.s.ld + col0;
 #pragma unroll
     for (int c0 = 0; c0 < NC; c0 += 32) {
       if (c0 < cols_left) {
         float x[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) x[c] = acc[c0 + c] * a.factor;
-        if constexpr (STAGE == kPolynomial || (STAGE == kMove && PARTS == 1)) {
-          uint32_t h[16];
-          take(hi_to, from, a.s.ld, c0, rows_left, a.s.ld - col0, h);
+        if constexpr (kReads) {
+          uint32_t h[16], l[16];
+          hand_out(hi_to, next.hi, h);
+          if constexpr (kReadsLow) hand_out(hi_to, next.lo, l);
+          if (c0 + 32 < NC) fetch(it, row0, col0 + c0 + 32, next);
           // of S b, with its diagonals apart b + c (D_i + D_j); of X the diagonal of P and a
           const auto weight = [&](int c) {
             if (STAGE == kPolynomial) return PARTS == 1 ? fmaf(a.factor, mine + __shfl_sync(0xffffffffu, theirs[c0 / 32], c), a.linear) : a.linear;
@@ -667,18 +690,13 @@ struct OrthogonalJob {
           };
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float2 v = floats(h[e]);
+            float2 v = floats(h[e]);
+            if constexpr (kReadsLow) {
+              const float2 low = floats(l[e]);
+              v = make_float2(fmaf(low.x, 0x1p-11f, v.x), fmaf(low.y, 0x1p-11f, v.y));
+            }
             x[2 * e] = fmaf(weight(2 * e), v.x, x[2 * e]);
             x[2 * e + 1] = fmaf(weight(2 * e + 1), v.y, x[2 * e + 1]);
-          }
-          if constexpr (PARTS == 2 || STAGE == kMove) {
-            take(hi_to, from + a.s.part, a.s.ld, c0, rows_left, a.s.ld - col0, h);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float2 v = floats(h[e]);
-              x[2 * e] = fmaf(weight(2 * e) * 0x1p-11f, v.x, x[2 * e]);
-              x[2 * e + 1] = fmaf(weight(2 * e + 1) * 0x1p-11f, v.y, x[2 * e + 1]);
-            }
           }
         }
         if (diagonal) {
@@ -775,6 +793,10 @@ cudaError_t launch(const typename J::Args& args, unsigned grid, const Room& room
   if (device > 63 || !(allowed.load() >> device & 1)) {
     e = cudaFuncSetAttribute(k_products<J>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
+    cudaFuncAttributes built;
+    e = cudaFuncGetAttributes(&built, k_products<J>);
+    if (e != cudaSuccess) return e;
+    if (J::kTma && built.numRegs < 168) return cudaErrorInvalidConfiguration;   // the registers that its warps share out (see k_products)
     if (device <= 63) allowed.fetch_or(1ull << device);
   }
   cudaLaunchConfig_t cfg{};

@@ -47,7 +47,7 @@ struct Geometry {
   static constexpr int kStage = PARTS * (kATile + kBTile);
   static constexpr int kStages = 196608 / kStage < 8 ? 196608 / kStage : 8;
   static constexpr int kProducers = TMA ? 1 : 8;               // warps
-  static constexpr int kThreads = (TMA ? kMmaWarp + 3 : kMmaWarp + kProducers) * 32;
+  static constexpr int kThreads = (TMA ? kMmaWarp + 4 : kMmaWarp + kProducers) * 32;
   static constexpr int kAccs = PARTS > 1 ? 2 : 1;              // accumulators of a set
   static constexpr uint32_t kTmemCols = 2 * kAccs * BN;
   static constexpr int kBuffersAt = kStages * kStage, kTablesAt = kBuffersAt + kEpiWarps * kBuffer;
@@ -145,6 +145,8 @@ __device__ __forceinline__ void copy_3d(uint32_t to, const CUtensorMap* map, int
                ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
+
+struct Nothing {};
 
 // What a block needs beside its operands.
 struct Bars {
@@ -308,7 +310,8 @@ struct Raw<unsigned short> {
 //   copy(item, chunk, tile, bar)      kTma: announces the bytes of this block's copies of a chunk at `bar` and issues them; template argument: whether `bar` is
 //                                     the first block's
 //   load_a, load_b(item, chunk, unit, raw)   otherwise: eight elements of a tile
-//   finish(item, acc, buf, warp)      the sums of this warp's rows and columns; by all epilogue warps
+//   early(item, warp, Early&)         loads of what finish() reads, issued before the sums are there
+//   finish(item, acc, Early&, buf, warp)   the sums of this warp's rows and columns; by all epilogue warps
 template <class J>
 using GeometryOf = Geometry<J::kParts, J::kBN, J::kTma, J::kPair>;
 
@@ -351,6 +354,12 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
     } else {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(G::kTmemCols) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  if constexpr (J::kTma) {
+    if (tid == kMmaWarp * 32 + 32) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&args.a) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&args.b) : "memory");
     }
   }
   gtc::enter_kernel();
@@ -400,6 +409,10 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
     }
   };
 
+  // Where copies go by TMA, of the registers of 384 threads (168 each) the epilogue's two groups of four warps get 208 and the
+  // others 80: 256 x 208 + 128 x 80 = 63488 of 64512.
+  if (warp >= kMmaWarp) {
+  if constexpr (J::kTma) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   if (warp == kMmaWarp + 2 && J::kTma) {
     if constexpr (J::kTma && J::kAMn) {
       // Rows of the next group come with the last chunk of a tile: the steps that are still read are cleared in both operands, in a pair by each
@@ -524,7 +537,9 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
         if (++slot == S) { slot = 0; parity ^= 1u; }
       }
     }
+  }
   } else {
+    if constexpr (J::kTma) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     constexpr int NC = BN / 2;   // columns of a warp
     constexpr float kCorrection = PARTS == 2 ? 0x1p-11f : 1.f;
     uint8_t* const buf = smem + G::kBuffersAt + warp * kBuffer;
@@ -537,6 +552,8 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
 #pragma unroll
       for (int c = 0; c < NC; ++c) acc[c] = 0.f;
       const bool mine = (warp >> 2) * NC < it.n;   // whether any of the warp's columns are asked for
+      typename J::Early early;
+      job.early(it, warp, early);
       for (int c = 0; c < it.chunks; c += segment) {
         ok = __all_sync(0xffffffffu, gtc::mbar_wait_abortable(acc_full + 8 * set, parity, abortp));
         if (!ok) break;
@@ -571,7 +588,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       }
       // where epilogue warps meet in finish(), those that gave up and those that did not leave together
       if constexpr (J::kMeets) ok = gtc::all_agree(ok, kEpiWarps * 32);
-      if (ok) job.finish(it, acc, buf, warp);
+      if (ok) job.finish(it, acc, early, buf, warp);
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
