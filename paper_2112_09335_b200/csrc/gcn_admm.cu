@@ -1947,11 +1947,12 @@ int gcn_admm_grouped_product(gcn_admm* h, int type, const void* x, long long ldx
     p.offsets = offsets_or_communities(h, offsets, n_groups, rows);
     if (rows == 0) return;
     h->need_device({x, w, y, offsets});
+    const gcn_admm_grouped::Room room = h->room_for(gcn_admm_grouped::space_bytes(p), 0);
     char name[48];
     std::snprintf(name, sizeof name, "grouped@%dx%d", k, n);
     const int size = gcn_admm_grouped::size_of(type);
     gcn_admm::Scope sc(h, name, 0, (double)rows * k * size + (double)n_groups * k * n * size + (double)rows * n * gcn_admm_grouped::size_of(out_type), 2.0 * (double)rows * k * n);
-    CU(gcn_admm_grouped::enqueue(p, gcn_admm_grouped::Room{nullptr, nullptr, h->tc_error, h->stream, &h->launches}));
+    CU(gcn_admm_grouped::enqueue(p, room));
   });
 }
 

@@ -18,6 +18,21 @@ __device__ __forceinline__ void put(float* at, float x) { *at = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* at, float x) { *at = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void put(__half* at, float x) { *at = __float2half_rn(x); }
 
+// Eight elements of a row, those from `valid` on zero.
+template <typename T>
+__device__ __forceinline__ void load8(const T* at, int valid, bool vec, float (&v)[8]) {
+  if (vec && valid >= 8) {
+    uint4 w[sizeof(T) / 2];
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) w[k] = *(reinterpret_cast<const uint4*>(at) + k);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = to_float(reinterpret_cast<const T*>(w)[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = k < valid ? to_float(at[k]) : 0.f;
+  }
+}
+
 constexpr int kSms = 148;
 
 // ---- groups of rows ----------------------------------------------------------------------------------
@@ -77,12 +92,35 @@ struct ProductArgs {
   bool vec_x, vec_w, vec_y;   // rows start on 16-byte boundaries
 };
 
-template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA, bool PAIR = false, bool VEC = false>
+// The weights of a product of many rows, fp32, as the three parts of their elements: images of part 0 of all matrices, then part 1 and 2, rows padded to 16
+// bytes, from which tiles are copied by TMA.  Otherwise every tile of 128 rows would split them again.
+struct SplitWeights {
+  const float* w;
+  long long ldw, stride_w;
+  int rows, cols, ld, groups;
+  bool vec;
+  unsigned short* to;
+};
+__global__ void __launch_bounds__(256) k_split_weights(const SplitWeights p) {
+  gtc::enter_kernel();
+  const unsigned units = p.ld / 8, count = (unsigned)p.rows * units;   // checked: below 2^31
+  const long long part = (long long)p.groups * p.rows * p.ld;
+  const float* const w = p.w + (long long)blockIdx.y * p.stride_w;
+  unsigned short* const to = p.to + (long long)blockIdx.y * p.rows * p.ld;
+  for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += gridDim.x * 256) {
+    const unsigned row = e / units, col = (e - row * units) * 8;
+    Raw<float> x;
+    load8(w + row * p.ldw + col, p.cols - (int)col, p.vec, x.x);
+    x.store(reinterpret_cast<uint8_t*>(to + (long long)row * p.ld + col), part * 2);
+  }
+}
+
+template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA, bool PAIR = false, bool VEC = false, bool SPLIT = false>
 struct ProductJob {
   using T = T_;
   using Args = ProductArgs;
   static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kMeets = false, kPair = PAIR;
+  static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kTmaB = SPLIT, kMeets = false, kPair = PAIR;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM;
   struct Item {
     int chunks, n, tail, g, row0, left, col0;
@@ -137,6 +175,20 @@ struct ProductJob {
       for (int b = 0; b < boxes; ++b) copy_3d<THERE>(tile + kATile + b * kGroup64, &a.b, col0 + 64 * b, c * kBK, it.g, bar);
     }
   }
+  __device__ __forceinline__ void copy_b(const Item& it, int c, uint32_t tile, uint32_t bar) const {
+    const int boxes = TRANSPOSED ? BN / 64 : min(BN / 64, (it.n + 63) / 64);
+    expect<false>(bar, (uint32_t)(PARTS * boxes * kGroup64));
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+      const uint32_t to = tile + part * (BN * kBK * 2);
+      const int z = part * groups.count + it.g;
+      if constexpr (TRANSPOSED) {
+        copy_3d<false>(to, &a.b, c * kBK, it.col0, z, bar);
+      } else {
+        for (int b = 0; b < boxes; ++b) copy_3d<false>(to + b * kGroup64, &a.b, it.col0 + 64 * b, c * kBK, z, bar);
+      }
+    }
+  }
   __device__ __forceinline__ void load_a(const Item& it, int c, int at, Raw<T>& raw) const {
     const int row = at >> 3, k = c * kBK + (at & 7) * 8;
     raw.template load<VEC>(static_cast<const T*>(a.p.x) + (long long)(it.row0 + row) * a.p.ldx + k, row < it.left ? a.p.k - k : 0);
@@ -189,7 +241,7 @@ struct ProductTnJob {
   using Args = ProductTnArgs;
   using Size = unsigned long long;
   static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kMeets = true, kPair = PAIR;
+  static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kTmaB = false, kMeets = true, kPair = PAIR;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kRanks = PAIR ? 2 : 1;
   struct Item {
     int chunks, n, tail, g, row0, end, m0, col0;
@@ -407,21 +459,6 @@ struct Image {
 
 constexpr int kNormBlocks = 256;   // partial sums of a norm, at most
 
-// Eight elements of a row, those from `valid` on zero.
-template <typename T>
-__device__ __forceinline__ void load8(const T* at, int valid, bool vec, float (&v)[8]) {
-  if (vec && valid >= 8) {
-    uint4 w[sizeof(T) / 2];
-#pragma unroll
-    for (int k = 0; k < (int)sizeof(T) / 2; ++k) w[k] = *(reinterpret_cast<const uint4*>(at) + k);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = to_float(reinterpret_cast<const T*>(w)[k]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < valid ? to_float(at[k]) : 0.f;
-  }
-}
-
 // Partial sums of squares of every matrix; in fp64: squares of fp32 numbers leave the range of fp32.  (One load a thread and 64 blocks took 520 us
 // of 4096 x 4096 halves, eight elements a load and as many blocks as there is work for WITH.)
 template <typename T>
@@ -516,7 +553,7 @@ template <Stage STAGE, int PARTS, int BN, bool A_MN, bool B_MN, bool PAIR>
 struct OrthogonalJob {
   using Args = OrthogonalArgs;
   static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
+  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kTmaB = false, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kBCols = PAIR ? BN / 2 : BN;
   struct Item {
     int chunks, n, tail, matrix, row0, col0;
@@ -893,6 +930,17 @@ struct OrthogonalSpace {
 };
 std::size_t space_bytes(const Orthogonal& p) { return OrthogonalSpace(p, nullptr).bytes; }
 
+// Whether the weights are split beforehand: where there are at least two tiles of rows to a group they are read again for every one (WITH).
+bool splits_weights(const Product& p) {
+  const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
+  return p.type == kF32 && p.rows >= 2LL * kBM * p.groups && w_rows * cdiv(w_cols, 8) < INT_MAX && gcn_admm_host::encode_tiled() != nullptr;
+}
+std::size_t space_bytes(const Product& p) {
+  if (!splits_weights(p)) return 0;
+  const std::size_t rows = p.transposed ? p.n : p.k, ld = cdiv(p.transposed ? p.k : p.n, 8) * 8;
+  return 3 * (std::size_t)p.groups * rows * ld * 2;
+}
+
 cudaError_t enqueue(const Product& p, const Room& room) {
   if (p.rows == 0) return cudaSuccess;
   ProductArgs a{};
@@ -908,12 +956,20 @@ cudaError_t enqueue(const Product& p, const Room& room) {
     if (make_map(&a.a, p.type, p.x, p.k, p.rows, p.ldx, 1, 0, kBM) && make_map(&a.b, p.type, p.w, w_cols, w_rows, p.ldw, p.groups, p.stride_w, p.transposed ? 128 : kBK))
       return p.transposed ? launch<ProductJob<unsigned short, 1, 256, true, true, true>>(a, kSms, room) : launch<ProductJob<unsigned short, 1, 256, false, true, true>>(a, kSms, room);
   }
-  const bool quads = a.vec_x && a.vec_w && p.k % 4 == 0 && (p.transposed || p.n % 4 == 0);   // rows of both operands are whole quads
+  const bool split = splits_weights(p);
+  const bool x_quads = a.vec_x && p.k % 4 == 0, quads = x_quads && a.vec_w && (p.transposed || p.n % 4 == 0);   // rows of the operands are whole quads
   const auto pick = [&](auto tma) {
     // The widest tile that still gives every SM one
     const auto enough = [&](int bn) { return p.n > bn / 2 && tiles_m * cdiv(p.n, bn) >= kSms; };
     const int bn = decltype(tma)::value && enough(256) ? 256 : enough(128) ? 128 : 64;
     const unsigned grid = (unsigned)std::min<long long>(kSms, tiles_m * cdiv(p.n, bn));
+    if (split) {
+      const int w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n, ld = (w_cols + 7) / 8 * 8;
+      const SplitWeights sw{static_cast<const float*>(p.w), p.ldw, p.stride_w, w_rows, w_cols, ld, p.groups, a.vec_w, static_cast<unsigned short*>(room.space)};
+      const cudaError_t e = launch_plain(k_split_weights, dim3((unsigned)std::min<long long>(256, cdiv((long long)w_rows * (ld / 8), 256)), (unsigned)p.groups), room, sw);
+      if (e != cudaSuccess) return e;
+      if (!make_map(&a.b, kBf16, room.space, w_cols, w_rows, ld, 3LL * p.groups, (long long)w_rows * ld, p.transposed ? bn : kBK)) return cudaErrorNotSupported;
+    }
     if (decltype(tma)::value) {
       const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
       if (!make_map(&a.a, p.type, p.x, p.k, p.rows, p.ldx, 1, 0, kBM) ||
@@ -925,6 +981,8 @@ cudaError_t enqueue(const Product& p, const Room& room) {
       constexpr bool T = decltype(turned)::value;
       if constexpr (decltype(tma)::value) return launch<ProductJob<unsigned short, 1, BN, T, true>>(a, grid, room);
       else if constexpr (BN == 256) return cudaErrorNotSupported;
+      else if (split && x_quads) return launch<ProductJob<float, 3, BN, T, false, false, true, true>>(a, grid, room);
+      else if (split) return launch<ProductJob<float, 3, BN, T, false, false, false, true>>(a, grid, room);
       else if (p.type == kF32 && quads) return launch<ProductJob<float, 3, BN, T, false, false, true>>(a, grid, room);
       else if (p.type == kF32) return launch<ProductJob<float, 3, BN, T, false>>(a, grid, room);
       else return launch<ProductJob<unsigned short, 1, BN, T, false>>(a, grid, room);

@@ -14,6 +14,7 @@ struct Room {
   cudaStream_t stream;
   long long* launches;   // counted up
 };
+std::size_t space_bytes(const Product& p);
 std::size_t space_bytes(const ProductTn& p);
 std::size_t tickets_of(const ProductTn& p);
 std::size_t space_bytes(const Orthogonal& p);

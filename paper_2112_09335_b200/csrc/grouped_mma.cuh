@@ -300,7 +300,7 @@ struct Raw<unsigned short> {
 };
 
 // The shared loop.  A job J says what the items are, where operand tiles come from and what becomes of a tile's sums:
-//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kPair, kMeets (finish() has barriers of the epilogue warps)
+//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kTmaB (of operands that go through registers B still comes by TMA), kPair, kMeets (finish() has barriers of the epilogue warps)
 //   segment()                         chunks of a segment, a power of two
 //   J(args, tables, rank)             built by every thread (rank: of the block in its pair); setup(): tables in shared memory, by the whole
 //                                     block, between barriers
@@ -309,7 +309,7 @@ struct Raw<unsigned short> {
 //                                     (steps of the last chunk that count, where rows behind them hold other data; else 64)
 //   copy(item, chunk, tile, bar)      kTma: announces the bytes of this block's copies of a chunk at `bar` and issues them; template argument: whether `bar` is
 //                                     the first block's
-//   load_a, load_b(item, chunk, unit, raw)   otherwise: eight elements of a tile
+//   load_a, load_b(item, chunk, unit, raw)   otherwise: eight elements of a tile; copy_b(item, chunk, tile, bar) where kTmaB
 //   early(item, warp, Early&)         loads of what finish() reads, issued before the sums are there
 //   finish(item, acc, Early&, buf, warp)   the sums of this warp's rows and columns; by all epilogue warps
 template <class J>
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   const uint32_t full_there = PAIR ? of_first_block(full) : full, acc_empty_there = PAIR ? of_first_block(acc_empty) : acc_empty;
   if (tid == 0) {
     for (int s = 0; s < S; ++s) {
-      gtc::mbar_init(full + 8 * s, PAIR ? 2 : G::kProducers);
+      gtc::mbar_init(full + 8 * s, PAIR ? 2 : G::kProducers + (J::kTmaB ? 1 : 0));
       gtc::mbar_init(empty + 8 * s, 1);
       gtc::mbar_init(tail + 8 * s, 1);
     }
@@ -459,60 +459,86 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
     }
   } else if (warp >= kMmaWarp && !J::kTma) {
     if constexpr (!J::kTma) {
+      // Elements are loaded kAhead chunks before they go to shared memory (two where B comes by TMA and leaves the registers): `next` and `coming` are the
+      // item and chunk of the loads, `it` and c those of the stores.
+      constexpr int kAhead = J::kTmaB ? 2 : 1, kUnitsA = kBM * 8 / 256, kUnitsB = J::kTmaB ? 0 : BN * 8 / 256;
       using R = Raw<typename J::T>;
-      R a[kBM * 8 / 256], b[BN * 8 / 256];
+      R a[kAhead][kUnitsA], b[kAhead][kUnitsB > 0 ? kUnitsB : 1];
       const int t = tid - kMmaWarp * 32;
-      int slot = 0, set = 0, c = 0;
+      int slot = 0, set = 0, c = 0, coming = 0;
       uint32_t parity = 1, acc_parity = 1;
-      bool more = job.next(walk, it);
-      const auto settle = [&] {   // on to the next item where this one has no chunk left
-        while (more && c >= it.chunks) {
-          c = 0;
-          more = job.next(walk, it);
+      typename J::Item next;
+      typename J::Walk ahead = walk;
+      const auto settle = [&](typename J::Walk& w, typename J::Item& item, int& chunk) {   // on to the next item where this one has no chunk left
+        while (chunk >= item.chunks) {
+          chunk = 0;
+          if (!job.next(w, item)) return false;
         }
+        return true;
       };
-      settle();
-      if (more) {
+      it.chunks = next.chunks = 0;
+      bool more = settle(walk, it, c), more_ahead = settle(ahead, next, coming);
 #pragma unroll
-        for (int u = 0; u < kBM * 8 / 256; ++u) job.load_a(it, c, t + 256 * u, a[u]);
+      for (int d = 0; d < kAhead; ++d) {
+        if (more_ahead) {
 #pragma unroll
-        for (int u = 0; u < BN * 8 / 256; ++u) job.load_b(it, c, t + 256 * u, b[u]);
+          for (int u = 0; u < kUnitsA; ++u) job.load_a(next, coming, t + 256 * u, a[d][u]);
+#pragma unroll
+          for (int u = 0; u < kUnitsB; ++u) job.load_b(next, coming, t + 256 * u, b[d][u]);
+          ++coming;
+          more_ahead = settle(ahead, next, coming);
+        }
       }
-      while (more) {
-        if (!__all_sync(0xffffffffu, gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp))) break;
-        uint8_t* const st = smem + (size_t)slot * G::kStage;
-        const bool first = (c & (segment - 1)) == 0, ends = c + 1 == it.chunks || (c & (segment - 1)) == segment - 1;
-        const int columns = it.n;
-        ++c;
-        settle();
-        // eight elements go to shared memory and those of the next chunk into their place: loads are on their way during all of this
+      bool ok = true;
+      while (ok && more) {
 #pragma unroll
-        for (int u = 0; u < kBM * 8 / 256; ++u) {
-          const int at = t + 256 * u;
-          a[u].store(st + (J::kAMn ? unit_mn(at / (kBM / 8), at % (kBM / 8)) : unit_k(at >> 3, at & 7)), kATile);
-          if (more) job.load_a(it, c, at, a[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < BN * 8 / 256; ++u) {
-          const int at = t + 256 * u;
-          b[u].store(st + PARTS * kATile + (J::kBMn ? unit_mn(at / (BN / 8), at % (BN / 8)) : unit_k(at >> 3, at & 7)), G::kBTile);
-          if (more) job.load_b(it, c, at, b[u]);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        gtc::mbar_arrive_warp(full + 8 * slot);
-        if (warp == kMmaWarp) {   // the others are about as far
-          if (!__all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
-                                           gtc::mbar_wait_abortable(full + 8 * slot, parity ^ 1u, abortp)))
-            break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          if (lane == 0) issue(slot, set, columns, kBK / 16, first, ends);
-          __syncwarp();
-          if (ends) {
-            if (set == 1) acc_parity ^= 1u;
-            set ^= 1;
+        for (int d = 0; d < kAhead; ++d) {
+          if (!more) break;
+          ok = __all_sync(0xffffffffu, gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp));
+          if (!ok) break;
+          uint8_t* const st = smem + (size_t)slot * G::kStage;
+          if constexpr (J::kTmaB) {
+            if (t == 32) {
+              job.copy_b(it, c, base + (uint32_t)(slot * G::kStage + PARTS * kATile), full + 8 * slot);
+              ++copies;
+            }
           }
+          // eight elements go to shared memory and those of a later chunk into their place: loads are on their way during all of this
+#pragma unroll
+          for (int u = 0; u < kUnitsA; ++u) {
+            const int at = t + 256 * u;
+            a[d][u].store(st + (J::kAMn ? unit_mn(at / (kBM / 8), at % (kBM / 8)) : unit_k(at >> 3, at & 7)), kATile);
+            if (more_ahead) job.load_a(next, coming, at, a[d][u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kUnitsB; ++u) {
+            const int at = t + 256 * u;
+            b[d][u].store(st + PARTS * kATile + (J::kBMn ? unit_mn(at / (BN / 8), at % (BN / 8)) : unit_k(at >> 3, at & 7)), G::kBTile);
+            if (more_ahead) job.load_b(next, coming, at, b[d][u]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          gtc::mbar_arrive_warp(full + 8 * slot);
+          const bool first = (c & (segment - 1)) == 0, ends = c + 1 == it.chunks || (c & (segment - 1)) == segment - 1;
+          if (warp == kMmaWarp) {   // the others are about as far
+            ok = __all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
+                                             gtc::mbar_wait_abortable(full + 8 * slot, parity ^ 1u, abortp));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (lane == 0) issue(slot, set, it.n, kBK / 16, first, ends);
+            __syncwarp();
+            if (ends) {
+              if (set == 1) acc_parity ^= 1u;
+              set ^= 1;
+            }
+          }
+          ++c;
+          more = settle(walk, it, c);
+          if (more_ahead) {
+            ++coming;
+            more_ahead = settle(ahead, next, coming);
+          }
+          if (++slot == S) { slot = 0; parity ^= 1u; }
         }
-        if (++slot == S) { slot = 0; parity ^= 1u; }
       }
     }
   } else if (warp == kMmaWarp) {
@@ -595,7 +621,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   __syncthreads();
   if (abort_flag) {   // what is still in flight is waited for before shared and tensor memory are let go
     if (tid == 0) atomicOr(job.error_flag(), 1);
-    if (warp == kMmaWarp + 1 && lane == 0 && J::kTma && rank == 0) gtc::drain_copies(full, S, copies);
+    if (warp == kMmaWarp + 1 && lane == 0 && (J::kTma || J::kTmaB) && rank == 0) gtc::drain_copies(full, S, copies);
     if (warp == kMmaWarp && lane == 0 && rank == 0) {
       if constexpr (PAIR) {
         commit_pair(drain);

@@ -147,6 +147,14 @@ def test_product_tn(h, kind, ka, nb):
         run_tn(h, sizes, ka, nb, kind, "f32" if i % 2 else kind, seed=i)
 
 
+@pytest.mark.parametrize("k, n", [(1, 1), (7, 5), (64, 40), (100, 256), (129, 70), (200, 130), (331, 264)])
+def test_fp32_product_of_many_rows(h, k, n):
+    """Enough rows to a group for its weights to be split once for all of them."""
+    for transposed in (False, True):
+        run_product(h, [1000, 0, 513], k, n, "f32", "f32", transposed, first=3, tail=9)
+        run_product(h, [700], k, n, "f32", "f32", transposed, x_pad=1, w_pad=3, y_pad=2, shift=1, gap=5)
+
+
 LAYOUTS = [dict(x_pad=8, y_pad=16, w_pad=8), dict(x_pad=3, y_pad=1, w_pad=5, gap=7), dict(shift=1), dict(shift=8, gap=8), dict(x_pad=4, y_pad=4, w_pad=4, shift=4)]
 
 
