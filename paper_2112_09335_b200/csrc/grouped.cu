@@ -62,23 +62,25 @@ __device__ __forceinline__ void scan(V* v, int count) {
   }
 }
 
-// Which item belongs to which group: every block counts for itself (1024 groups are 4 loads a thread and a scan by one warp; a launch
+// Rows of the groups, and tiles of rows: every block counts for itself (1024 groups are 4 loads a thread and a scan by one warp; a launch
 // that wrote the table down would cost more than all blocks' counting).
 struct Groups {
-  unsigned* ends;     // [groups] items of this group and all before it
+  unsigned* ends;     // [groups] tiles of rows of this group and all before it
   int *begin, *end;   // [groups] rows
   int count;
   __device__ __forceinline__ Groups(uint8_t* tables, int count_)
       : ends(reinterpret_cast<unsigned*>(tables)), begin(reinterpret_cast<int*>(tables) + kMaxGroups), end(reinterpret_cast<int*>(tables) + 2 * kMaxGroups), count(count_) {}
-  // The group of item i < ends[count - 1], from `g` on; `before`: items ahead of it.
-  __device__ __forceinline__ int find(unsigned i, unsigned& before) const {
-    int lo = 0, hi = count - 1;
+  __device__ __forceinline__ unsigned tiles() const { return ends[count - 1]; }
+  // The group of tile i < tiles(), from g on.
+  __device__ __forceinline__ int find(unsigned i, int g) const {
+    for (int k = 0; k < 3; ++k, ++g)   // mostly this group or one of the next
+      if (ends[g] > i) return g;
+    int lo = g, hi = count - 1;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (ends[mid] > i) hi = mid;
       else lo = mid + 1;
     }
-    before = lo > 0 ? ends[lo - 1] : 0u;
     return lo;
   }
 };
@@ -138,28 +140,38 @@ struct ProductJob {
       const int2 r = group_rows(a.p.offsets, g, (int)a.p.rows);
       groups.begin[g] = r.x;
       groups.end[g] = r.y;
-      groups.ends[g] = (unsigned)min((unsigned long long)((r.y - r.x + kTileRows - 1) / kTileRows) * tiles_n, (unsigned long long)INT_MAX);
+      groups.ends[g] = (unsigned)((r.y - r.x + kTileRows - 1) / kTileRows);
     }
     __syncthreads();
     if (threadIdx.x < 32) scan(groups.ends, groups.count);
   }
+  // Tiles in turn, those of a row of tiles one after the other.  The next is step tiles on: step_rows rows of tiles and step_cols of the row.  (With the group searched for and
+  // divisions on every step it took a thousand clocks.)
   struct Walk {
-    unsigned i, step;
+    unsigned row, col, step_rows, step_cols;
+    int g;
   };
-  __device__ __forceinline__ Walk start(unsigned worker, unsigned workers) const { return Walk{worker, workers}; }
+  __device__ __forceinline__ Walk start(unsigned worker, unsigned workers) const {
+    const unsigned n = (unsigned)tiles_n;
+    return Walk{worker / n, worker % n, workers / n, workers % n, 0};
+  }
   __device__ __forceinline__ bool next(Walk& at, Item& it) const {
-    const unsigned i = at.i;
-    if (i >= groups.ends[groups.count - 1]) return false;
-    at.i += at.step;
-    unsigned before;
-    it.g = groups.find(i, before);
-    const unsigned local = i - before, tile = local / tiles_n;
-    it.row0 = groups.begin[it.g] + (int)tile * kTileRows + rank * kBM;
-    it.left = groups.end[it.g] - it.row0;
-    it.col0 = (int)(local - tile * tiles_n) * BN;
+    if (at.row >= groups.tiles()) return false;
+    at.g = groups.find(at.row, at.g);
+    const unsigned before = at.g > 0 ? groups.ends[at.g - 1] : 0u;
+    it.g = at.g;
+    it.row0 = groups.begin[at.g] + (int)(at.row - before) * kTileRows + rank * kBM;
+    it.left = groups.end[at.g] - it.row0;
+    it.col0 = (int)at.col * BN;
     it.n = a.p.n - it.col0;
     it.chunks = (a.p.k + kBK - 1) / kBK;
     it.tail = kBK;
+    at.row += at.step_rows;
+    at.col += at.step_cols;
+    if (at.col >= (unsigned)tiles_n) {
+      at.col -= tiles_n;
+      ++at.row;
+    }
     return true;
   }
   template <bool THERE>
@@ -833,7 +845,7 @@ cudaError_t launch(const typename J::Args& args, unsigned grid, const Room& room
     cudaFuncAttributes built;
     e = cudaFuncGetAttributes(&built, k_products<J>);
     if (e != cudaSuccess) return e;
-    if (J::kTma && built.numRegs < 168) return cudaErrorInvalidConfiguration;   // the registers that its warps share out (see k_products)
+    if (built.numRegs < (J::kTma ? 168 : 96)) return cudaErrorInvalidConfiguration;   // the registers that its warps share out (see k_products)
     if (device <= 63) allowed.fetch_or(1ull << device);
   }
   cudaLaunchConfig_t cfg{};

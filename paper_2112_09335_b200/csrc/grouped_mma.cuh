@@ -3,8 +3,10 @@
 // A block owns one SM and walks over work items, each a tile of 128 rows x kBN columns of some D = A B with a reduction of any length.
 //   warps 0-7    epilogue: tensor memory -> registers -> sums of segments -> result
 //   warp 8       matrix instructions (one lane issues)
-//   warp 9       copies of operand tiles by TMA (warp 10: clears what they bring from behind the end of a group), or warps 8-15: operand tiles through registers (warp 8 issues behind its part of a chunk; as a 17th
-//                warp the issuer left 96 registers a thread, too few for a chunk in flight)
+//   warp 9       copies of operand tiles by TMA;  warp 10: clears what they bring from behind the end of a group
+//   warps 12-19  where an operand has to be split or does not lie on 16-byte boundaries: its tiles, through registers
+// (Issuing behind a producer's part of a chunk, in 16 warps, held up that warp and with it all others: 24 instructions take 2600 clocks to
+// be accepted.)
 // Operand tiles are 64 steps of the reduction wide and lie in shared memory with the 128-byte swizzle, K-major (a row of the tile is
 // 128 bytes of the reduction) or MN-major (a row is one step of the reduction, 128 bytes of the tile's rows or columns; tiles of more than 64 are
 // groups of 64, 8192 bytes apart), whichever way the matrix lies in memory: nothing is ever transposed by hand.
@@ -37,7 +39,7 @@ using gtc::smem_u32;
 constexpr int kBM = 128, kBK = 64;   // rows of a tile; reduction steps of a chunk
 constexpr int kATile = kBM * kBK * 2;              // bytes of one part of an operand tile of A
 constexpr int kGroup64 = kBK * 128;                // bytes between groups of 64 in an MN-major tile
-constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps;
+constexpr int kEpiWarps = 8, kMmaWarp = kEpiWarps, kFirstLoader = kMmaWarp + 4;
 constexpr int kBuffer = 2048;                      // bytes of an epilogue warp's buffer: 32 rows of 64
 
 template <int PARTS, int BN, bool TMA, bool PAIR>
@@ -47,7 +49,7 @@ struct Geometry {
   static constexpr int kStage = PARTS * (kATile + kBTile);
   static constexpr int kStages = 196608 / kStage < 8 ? 196608 / kStage : 8;
   static constexpr int kProducers = TMA ? 1 : 8;               // warps
-  static constexpr int kThreads = (TMA ? kMmaWarp + 4 : kMmaWarp + kProducers) * 32;
+  static constexpr int kThreads = (kMmaWarp + 4 + (TMA ? 0 : kProducers)) * 32;
   static constexpr int kAccs = PARTS > 1 ? 2 : 1;              // accumulators of a set
   static constexpr uint32_t kTmemCols = 2 * kAccs * BN;
   static constexpr int kBuffersAt = kStages * kStage, kTablesAt = kBuffersAt + kEpiWarps * kBuffer;
@@ -356,11 +358,9 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
   }
-  if constexpr (J::kTma) {
-    if (tid == kMmaWarp * 32 + 32) {
-      asm volatile("prefetch.tensormap [%0];" ::"l"(&args.a) : "memory");
-      asm volatile("prefetch.tensormap [%0];" ::"l"(&args.b) : "memory");
-    }
+  if (tid == kMmaWarp * 32 + 32) {
+    if constexpr (J::kTma) asm volatile("prefetch.tensormap [%0];" ::"l"(&args.a) : "memory");
+    if constexpr (J::kTma || J::kTmaB) asm volatile("prefetch.tensormap [%0];" ::"l"(&args.b) : "memory");
   }
   gtc::enter_kernel();
   J job(args, smem + G::kTablesAt, rank);
@@ -409,10 +409,12 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
     }
   };
 
-  // Where copies go by TMA, of the registers of 384 threads (168 each) the epilogue's two groups of four warps get 208 and the
-  // others 80: 256 x 208 + 128 x 80 = 63488 of 64512.
-  if (warp >= kMmaWarp) {
+  // Registers go where they are needed.  384 threads start with 168 each: the epilogue's eight warps get 208, the four others 80 (256 x 208 + 128 x 80 = 63488
+  // of 64512).  640 threads start with 96: the epilogue gets 104, the eight loading warps 112 and the four others 48 (256 x 104 + 256 x 112 + 128 x 48 = 61440,
+  // all there are).
+  if (warp >= kMmaWarp && warp < kFirstLoader) {
   if constexpr (J::kTma) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
   if (warp == kMmaWarp + 2 && J::kTma) {
     if constexpr (J::kTma && J::kAMn) {
       // Rows of the next group come with the last chunk of a tile: the steps that are still read are cleared in both operands, in a pair by each
@@ -437,10 +439,10 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
         else gtc::mbar_arrive_warp(full + 8 * at);
       }
     }
-  } else if (warp == kMmaWarp + 1 && J::kTma) {
+  } else if (warp == kMmaWarp + 1 && (J::kTma || J::kTmaB)) {
     int slot = 0;
     uint32_t parity = 1;   // a fresh barrier passes a wait on parity 1
-    if constexpr (J::kTma) {
+    if constexpr (J::kTma || J::kTmaB) {
       if (lane == 0) {
         bool ok = true;
         while (ok && job.next(walk, it)) {
@@ -448,96 +450,13 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
             ok = gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp);
             if (!ok) break;
             const uint32_t tile = base + (uint32_t)slot * G::kStage;
+            if constexpr (J::kTmaB) job.copy_b(it, c, tile + PARTS * kATile, full + 8 * slot);
             // a chunk with rows to clear is announced to the warp that does it
-            if (J::kAMn && it.tail < kBK && c + 1 == it.chunks) job.template copy<false>(it, c, tile, tail + 8 * slot);
+            else if (J::kAMn && it.tail < kBK && c + 1 == it.chunks) job.template copy<false>(it, c, tile, tail + 8 * slot);
             else job.template copy<PAIR>(it, c, tile, full_there + 8 * slot);
             ++copies;
             if (++slot == S) { slot = 0; parity ^= 1u; }
           }
-        }
-      }
-    }
-  } else if (warp >= kMmaWarp && !J::kTma) {
-    if constexpr (!J::kTma) {
-      // Elements are loaded kAhead chunks before they go to shared memory (two where B comes by TMA and leaves the registers): `next` and `coming` are the
-      // item and chunk of the loads, `it` and c those of the stores.
-      constexpr int kAhead = J::kTmaB ? 2 : 1, kUnitsA = kBM * 8 / 256, kUnitsB = J::kTmaB ? 0 : BN * 8 / 256;
-      using R = Raw<typename J::T>;
-      R a[kAhead][kUnitsA], b[kAhead][kUnitsB > 0 ? kUnitsB : 1];
-      const int t = tid - kMmaWarp * 32;
-      int slot = 0, set = 0, c = 0, coming = 0;
-      uint32_t parity = 1, acc_parity = 1;
-      typename J::Item next;
-      typename J::Walk ahead = walk;
-      const auto settle = [&](typename J::Walk& w, typename J::Item& item, int& chunk) {   // on to the next item where this one has no chunk left
-        while (chunk >= item.chunks) {
-          chunk = 0;
-          if (!job.next(w, item)) return false;
-        }
-        return true;
-      };
-      it.chunks = next.chunks = 0;
-      bool more = settle(walk, it, c), more_ahead = settle(ahead, next, coming);
-#pragma unroll
-      for (int d = 0; d < kAhead; ++d) {
-        if (more_ahead) {
-#pragma unroll
-          for (int u = 0; u < kUnitsA; ++u) job.load_a(next, coming, t + 256 * u, a[d][u]);
-#pragma unroll
-          for (int u = 0; u < kUnitsB; ++u) job.load_b(next, coming, t + 256 * u, b[d][u]);
-          ++coming;
-          more_ahead = settle(ahead, next, coming);
-        }
-      }
-      bool ok = true;
-      while (ok && more) {
-#pragma unroll
-        for (int d = 0; d < kAhead; ++d) {
-          if (!more) break;
-          ok = __all_sync(0xffffffffu, gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp));
-          if (!ok) break;
-          uint8_t* const st = smem + (size_t)slot * G::kStage;
-          if constexpr (J::kTmaB) {
-            if (t == 32) {
-              job.copy_b(it, c, base + (uint32_t)(slot * G::kStage + PARTS * kATile), full + 8 * slot);
-              ++copies;
-            }
-          }
-          // eight elements go to shared memory and those of a later chunk into their place: loads are on their way during all of this
-#pragma unroll
-          for (int u = 0; u < kUnitsA; ++u) {
-            const int at = t + 256 * u;
-            a[d][u].store(st + (J::kAMn ? unit_mn(at / (kBM / 8), at % (kBM / 8)) : unit_k(at >> 3, at & 7)), kATile);
-            if (more_ahead) job.load_a(next, coming, at, a[d][u]);
-          }
-#pragma unroll
-          for (int u = 0; u < kUnitsB; ++u) {
-            const int at = t + 256 * u;
-            b[d][u].store(st + PARTS * kATile + (J::kBMn ? unit_mn(at / (BN / 8), at % (BN / 8)) : unit_k(at >> 3, at & 7)), G::kBTile);
-            if (more_ahead) job.load_b(next, coming, at, b[d][u]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          gtc::mbar_arrive_warp(full + 8 * slot);
-          const bool first = (c & (segment - 1)) == 0, ends = c + 1 == it.chunks || (c & (segment - 1)) == segment - 1;
-          if (warp == kMmaWarp) {   // the others are about as far
-            ok = __all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
-                                             gtc::mbar_wait_abortable(full + 8 * slot, parity ^ 1u, abortp));
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (lane == 0) issue(slot, set, it.n, kBK / 16, first, ends);
-            __syncwarp();
-            if (ends) {
-              if (set == 1) acc_parity ^= 1u;
-              set ^= 1;
-            }
-          }
-          ++c;
-          more = settle(walk, it, c);
-          if (more_ahead) {
-            ++coming;
-            more_ahead = settle(ahead, next, coming);
-          }
-          if (++slot == S) { slot = 0; parity ^= 1u; }
         }
       }
     }
@@ -548,7 +467,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
     while (ok && job.next(walk, it)) {
       for (int c = 0; c < it.chunks; ++c) {
         const bool first = (c & (segment - 1)) == 0, last = c + 1 == it.chunks, ends = last || (c & (segment - 1)) == segment - 1;
-        const bool clears = J::kAMn && last && it.tail < kBK;
+        const bool clears = J::kTma && J::kAMn && last && it.tail < kBK;
         ok = __all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
                                          gtc::mbar_wait_abortable(full + 8 * slot, parity, abortp));
         if (!ok) break;
@@ -564,8 +483,63 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       }
     }
   }
+  } else if (warp >= kFirstLoader) {
+    if constexpr (!J::kTma) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+      // Elements are loaded kAhead chunks before they go to shared memory (two where B comes by TMA and leaves the registers).
+      constexpr int kAhead = J::kTmaB ? 2 : 1, kUnitsA = kBM * 8 / 256, kUnitsB = J::kTmaB ? 0 : BN * 8 / 256;
+      using R = Raw<typename J::T>;
+      R a[kAhead][kUnitsA], b[kAhead][kUnitsB > 0 ? kUnitsB : 1];
+      const int t = tid - kFirstLoader * 32;
+      int slot = 0, c = 0, held = 0;   // held: chunks in registers
+      uint32_t parity = 1;
+      it.chunks = 0;
+      const auto load = [&](R (&to_a)[kUnitsA], R (&to_b)[kUnitsB > 0 ? kUnitsB : 1]) {
+        while (c >= it.chunks) {   // on to the next item where this one has no chunk left
+          c = 0;
+          if (!job.next(walk, it)) {
+            it.chunks = 0;
+            return;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnitsA; ++u) job.load_a(it, c, t + 256 * u, to_a[u]);
+#pragma unroll
+        for (int u = 0; u < kUnitsB; ++u) job.load_b(it, c, t + 256 * u, to_b[u]);
+        ++c;
+        ++held;
+      };
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) load(a[d], b[d]);
+      bool ok = true;
+      while (ok && held > 0) {
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d) {
+          if (held == 0) break;
+          ok = __all_sync(0xffffffffu, gtc::mbar_wait_abortable(empty + 8 * slot, parity, abortp));
+          if (!ok) break;
+          uint8_t* const st = smem + (size_t)slot * G::kStage;
+#pragma unroll
+          for (int u = 0; u < kUnitsA; ++u) {
+            const int at = t + 256 * u;
+            a[d][u].store(st + (J::kAMn ? unit_mn(at / (kBM / 8), at % (kBM / 8)) : unit_k(at >> 3, at & 7)), kATile);
+          }
+#pragma unroll
+          for (int u = 0; u < kUnitsB; ++u) {
+            const int at = t + 256 * u;
+            b[d][u].store(st + PARTS * kATile + (J::kBMn ? unit_mn(at / (BN / 8), at % (BN / 8)) : unit_k(at >> 3, at & 7)), G::kBTile);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          gtc::mbar_arrive_warp(full + 8 * slot);
+          --held;
+          load(a[d], b[d]);
+          if (++slot == S) { slot = 0; parity ^= 1u; }
+        }
+      }
+    }
   } else {
     if constexpr (J::kTma) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     constexpr int NC = BN / 2;   // columns of a warp
     constexpr float kCorrection = PARTS == 2 ? 0x1p-11f : 1.f;
     uint8_t* const buf = smem + G::kBuffersAt + warp * kBuffer;
