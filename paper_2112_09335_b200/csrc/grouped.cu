@@ -544,6 +544,125 @@ __global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, con
   }
 }
 
+// Matrices whose shorter side is at most 32, all steps in one launch: a block has a matrix in its shared memory, in fp32 and with fp32 FMA.  (Through the tensor cores
+// every step is three launches of tiles that are nearly empty: eight matrices of 128 x 16 took 73 us, WITH us so.)
+// X lies as [n][M], its shorter side, padded to M, contiguous.  S: every warp adds up the products of its part of the n steps, a lane the M / 8 x M / 4
+// entries at its place, and the warps' sums are added in order.  X <- P X: a thread has columns of its own and reads P, the same for all.
+struct SmallSteps {
+  int count;
+  float c[3 * kMaxSteps];
+};
+constexpr int kSmallSide = 32, kSmallThreads = 512, kSmallBytes = 160 * 1024;
+template <int M>
+constexpr size_t small_bytes(int n) {
+  return ((size_t)n * M + (kSmallThreads / 32) * M * M + 2 * M * M) * sizeof(float);
+}
+template <int M, typename T, typename O>
+__global__ void __launch_bounds__(kSmallThreads) k_small(const Orthogonal p, const __grid_constant__ SmallSteps steps) {
+  gtc::enter_kernel();
+  constexpr int kWarps = kSmallThreads / 32, TI = M / 8, TJ = M / 4;
+  extern __shared__ __align__(16) float small_smem[];
+  __shared__ double s_sum[kWarps];
+  const bool tall = p.rows > p.cols;
+  const int m = tall ? p.cols : p.rows, n = tall ? p.rows : p.cols, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  float* const x = small_smem;
+  float* const part = x + (size_t)n * M;               // [kWarps][M][M]
+  float *const s = part + kWarps * M * M, *const f = s + M * M;
+  const T* const g = static_cast<const T*>(p.g) + (long long)blockIdx.x * p.stride_g;
+  const auto index = [&](int e, int& i, int& k) {      // of the e-th element as it lies in memory
+    const int row = e / p.cols, col = e - row * p.cols;
+    i = tall ? col : row;
+    k = tall ? row : col;
+    return row * p.ldg + col;
+  };
+  for (int e = tid; e < n * M; e += kSmallThreads) x[e] = 0.f;
+  __syncthreads();
+  double sum = 0.0;
+  for (int e = tid; e < m * n; e += kSmallThreads) {
+    int i, k;
+    const float v = to_float(g[index(e, i, k)]);
+    x[k * M + i] = v;
+    sum = fma((double)v, (double)v, sum);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0) s_sum[warp] = sum;
+  __syncthreads();
+  sum = 0.0;
+  for (int w = 0; w < kWarps; ++w) sum += s_sum[w];
+  const double norm = sqrt(sum) + (double)p.eps;
+  const double inverse = !(norm > 0.0) ? (sum == 0.0 ? 0.0 : nan("")) : norm < INFINITY ? 1.0 / norm : nan("");   // as k_start
+  for (int e = tid; e < n * M; e += kSmallThreads) x[e] = (float)((double)x[e] * (e % M < m ? inverse : 0.0));
+  __syncthreads();
+  for (int step = 0; step < steps.count; ++step) {
+    const float a = steps.c[3 * step], b = steps.c[3 * step + 1], c = steps.c[3 * step + 2];
+    {
+      const int i0 = (lane & 7) * TI, j0 = (lane >> 3) * TJ;
+      float acc[TI][TJ] = {};
+      for (int k = warp; k < n; k += kWarps) {
+        float u[TI], v[TJ];
+#pragma unroll
+        for (int i = 0; i < TI; ++i) u[i] = x[k * M + i0 + i];
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) v[j] = x[k * M + j0 + j];
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+          for (int j = 0; j < TJ; ++j) acc[i][j] = fmaf(u[i], v[j], acc[i][j]);
+      }
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) part[warp * M * M + (i0 + i) * M + j0 + j] = acc[i][j];
+    }
+    __syncthreads();
+    for (int e = tid; e < M * M; e += kSmallThreads) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) v += part[w * M * M + e];
+      s[e] = v;
+    }
+    __syncthreads();
+    for (int e = tid; e < M * M; e += kSmallThreads) {
+      const int i = e / M, j = e % M;
+      float v = 0.f;
+#pragma unroll
+      for (int q = 0; q < M; ++q) v = fmaf(s[i * M + q], s[q * M + j], v);
+      f[e] = fmaf(c, v, fmaf(b, s[e], i == j ? a : 0.f));
+    }
+    __syncthreads();
+    for (int k = tid; k < n; k += kSmallThreads) {
+      float v[M];
+#pragma unroll
+      for (int q = 0; q < M; q += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(x + k * M + q);
+        v[q] = w.x; v[q + 1] = w.y; v[q + 2] = w.z; v[q + 3] = w.w;
+      }
+#pragma unroll 4
+      for (int i = 0; i < M; ++i) {
+        float w[4] = {};
+#pragma unroll
+        for (int q = 0; q < M; q += 4) {
+          const float4 h = *reinterpret_cast<const float4*>(f + i * M + q);
+          w[0] = fmaf(h.x, v[q], w[0]);
+          w[1] = fmaf(h.y, v[q + 1], w[1]);
+          w[2] = fmaf(h.z, v[q + 2], w[2]);
+          w[3] = fmaf(h.w, v[q + 3], w[3]);
+        }
+        x[k * M + i] = (w[0] + w[1]) + (w[2] + w[3]);
+      }
+    }
+    __syncthreads();
+  }
+  O* const out = static_cast<O*>(p.out) + (long long)blockIdx.x * p.stride_o;
+  for (int e = tid; e < m * n; e += kSmallThreads) {
+    int i, k;
+    index(e, i, k);
+    const int row = tall ? k : i, col = tall ? i : k;
+    put(out + row * p.ldo + col, p.scale * x[k * M + i]);
+  }
+}
+
 enum Stage { kGram, kPolynomial, kMove };
 struct OrthogonalArgs {
   CUtensorMap a, b;
@@ -865,12 +984,13 @@ cudaError_t launch(const typename J::Args& args, unsigned grid, const Room& room
   return cudaLaunchKernelEx(&cfg, k_products<J>, args);
 }
 
-// The small kernels of 256 threads, launched the same way.
+// The small kernels, launched the same way.
 template <typename... P, typename... Q>
-cudaError_t launch_plain(void (*kernel)(P...), dim3 grid, const Room& room, const Q&... args) {
+cudaError_t launch_plain_of(void (*kernel)(P...), dim3 grid, int threads, size_t smem, const Room& room, const Q&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(256);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = room.stream;
   cudaLaunchAttribute behind{};
   behind.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -878,7 +998,11 @@ cudaError_t launch_plain(void (*kernel)(P...), dim3 grid, const Room& room, cons
   cfg.attrs = &behind;
   cfg.numAttrs = 1;
   ++*room.launches;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+  return cudaLaunchKernelEx(&cfg, kernel, std::remove_reference_t<P>(args)...);
+}
+template <typename... P, typename... Q>
+cudaError_t launch_plain(void (*kernel)(P...), dim3 grid, const Room& room, const Q&... args) {
+  return launch_plain_of(kernel, grid, 256, 0, room, args...);
 }
 template <typename T>
 struct Tag {
@@ -940,7 +1064,8 @@ struct OrthogonalSpace {
     bytes = used;
   }
 };
-std::size_t space_bytes(const Orthogonal& p) { return OrthogonalSpace(p, nullptr).bytes; }
+bool is_small(const Orthogonal& p);
+std::size_t space_bytes(const Orthogonal& p) { return is_small(p) ? 0 : OrthogonalSpace(p, nullptr).bytes; }
 
 // Whether the weights are split beforehand: where there are at least two tiles of rows to a group they are read again for every one (WITH).
 bool splits_weights(const Product& p) {
@@ -1041,8 +1166,29 @@ cudaError_t enqueue(const ProductTn& p, const Room& room) {
   });
 }
 
+// One block a matrix, where it fits (see k_small).
+bool is_small(const Orthogonal& p) {
+  const int m = std::min(p.rows, p.cols), n = std::max(p.rows, p.cols);
+  return m <= kSmallSide && (m <= 8 ? small_bytes<8>(n) : m <= 16 ? small_bytes<16>(n) : small_bytes<32>(n)) <= (size_t)kSmallBytes;
+}
+template <int M>
+cudaError_t enqueue_small(const Orthogonal& p, const Room& room) {
+  SmallSteps steps{};
+  steps.count = p.steps;
+  if (p.steps > 0) std::copy(p.coefficients, p.coefficients + 3 * p.steps, steps.c);
+  const size_t smem = small_bytes<M>(std::max(p.rows, p.cols));
+  cudaError_t e = cudaSuccess;
+  with_types(p.type, p.out_type, [&](auto in, auto out) {
+    const auto kernel = k_small<M, decltype(in), decltype(out)>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallBytes);
+    if (e == cudaSuccess) e = launch_plain_of(kernel, dim3((unsigned)p.batch), kSmallThreads, smem, room, p, steps);
+  });
+  return e;
+}
+
 cudaError_t enqueue(const Orthogonal& p, const Room& room) {
   const int m = std::min(p.rows, p.cols);
+  if (is_small(p)) return m <= 8 ? enqueue_small<8>(p, room) : m <= 16 ? enqueue_small<16>(p, room) : enqueue_small<32>(p, room);
   const bool tall = p.rows > p.cols;
   const OrthogonalSpace at(p, room.space);
   const Image none{nullptr, p.rows, at.x[0].ld, 0};

@@ -415,7 +415,8 @@ def ortho_tolerance(g, coefficients, dtype, eps=1e-7):
 
 @pytest.mark.parametrize("kind", NAMES)
 @pytest.mark.parametrize("batch, rows, cols", [(1, 1, 1), (2, 1, 9), (3, 5, 1), (5, 16, 7), (8, 128, 16), (2, 64, 64), (1, 65, 130), (3, 100, 47),
-                                               (1, 128, 256), (2, 129, 128), (1, 257, 300), (1, 500, 128), (1, 300, 767)])
+                                               (1, 128, 256), (2, 129, 128), (1, 257, 300), (1, 500, 128), (1, 300, 767),
+                                               (4, 8, 5000), (3, 32, 1100), (3, 1000, 31), (2, 2000, 16), (2, 33, 1000), (2, 24, 1500), (300, 12, 20)])
 def test_orthogonalise(h, kind, batch, rows, cols):
     import torch
     for out in {kind, "f32"}:
