@@ -88,7 +88,7 @@ constexpr int kTableBytes = 4 * kMaxGroups * 4 + 16 + (kSms + 1) * 8;
 
 // ---- y = x W_g ---------------------------------------------------------------------------------------
 struct ProductArgs {
-  CUtensorMap a, b;      // of x and of the weights, where tiles are copied by TMA
+  CUtensorMap a, b, few;   // of x and of the weights, where tiles are copied by TMA; of x in boxes of kFewRows rows
   Product p;
   int* error_flag;
   bool vec_x, vec_w, vec_y;   // rows start on 16-byte boundaries
@@ -116,6 +116,8 @@ __global__ void __launch_bounds__(256) k_split_weights(const SplitWeights p) {
     x.store(reinterpret_cast<uint8_t*>(to + (long long)row * p.ld + col), part * 2);
   }
 }
+
+constexpr int kFewRows = 16;   // (whole groups of eight rows of a tile)
 
 template <typename T_, int PARTS, int BN, bool TRANSPOSED, bool TMA, bool PAIR = false, bool VEC = false, bool SPLIT = false>
 struct ProductJob {
@@ -179,8 +181,15 @@ struct ProductJob {
     constexpr int kBCols = PAIR ? BN / 2 : BN;
     const int col0 = it.col0 + rank * kBCols;
     const int boxes = TRANSPOSED ? kBCols / 64 : min(kBCols / 64, max(0, (a.p.n - col0 + 63) / 64));   // columns behind the last are left out: they meet no result
-    expect<THERE>(bar, (uint32_t)(kATile + boxes * kGroup64));
-    copy_2d<THERE>(tile, &a.a, c * kBK, it.row0, bar);
+    // a group's last rows, of single tokens all it has, come without the rows behind them; what else is in the tile meets no result
+    const int few = PAIR ? kBM : (it.left + kFewRows - 1) / kFewRows;
+    if (few * kFewRows <= kBM / 2) {
+      expect<THERE>(bar, (uint32_t)(few * kFewRows * 128 + boxes * kGroup64));
+      for (int i = 0; i < few; ++i) copy_2d<THERE>(tile + i * kFewRows * 128, &a.few, c * kBK, it.row0 + i * kFewRows, bar);
+    } else {
+      expect<THERE>(bar, (uint32_t)(kATile + boxes * kGroup64));
+      copy_2d<THERE>(tile, &a.a, c * kBK, it.row0, bar);
+    }
     if constexpr (TRANSPOSED) {
       copy_3d<THERE>(tile + kATile, &a.b, c * kBK, col0, it.g, bar);
     } else {
@@ -1096,9 +1105,12 @@ cudaError_t enqueue(const Product& p, const Room& room) {
   const bool split = splits_weights(p);
   const bool x_quads = a.vec_x && p.k % 4 == 0, quads = x_quads && a.vec_w && (p.transposed || p.n % 4 == 0);   // rows of the operands are whole quads
   const auto pick = [&](auto tma) {
-    // The widest tile that still gives every SM one
-    const auto enough = [&](int bn) { return p.n > bn / 2 && tiles_m * cdiv(p.n, bn) >= kSms; };
-    const int bn = decltype(tma)::value && enough(256) ? 256 : enough(128) ? 128 : 64;
+    // A tile costs its columns, and its 128 rows as much as 64 columns; what counts are the tiles that one SM has.  (Eight rows of 64 groups, 1024 x 2048: 256 tiles of
+    // 64 columns, two for some SMs, WAS us, 128 of 128 columns WITH.)
+    const auto cost = [&](int bn) { return cdiv(tiles_m * cdiv(p.n, bn), kSms) * (std::min(bn, p.n) + 64); };
+    int bn = cost(128) <= cost(64) ? 128 : 64;
+    if (decltype(tma)::value && cost(256) <= cost(bn)) bn = 256;
+    if (p.n <= bn / 2) bn = p.n <= 64 ? 64 : 128;
     const unsigned grid = (unsigned)std::min<long long>(kSms, tiles_m * cdiv(p.n, bn));
     if (split) {
       const int w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n, ld = (w_cols + 7) / 8 * 8;
@@ -1109,7 +1121,7 @@ cudaError_t enqueue(const Product& p, const Room& room) {
     }
     if (decltype(tma)::value) {
       const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
-      if (!make_map(&a.a, p.type, p.x, p.k, p.rows, p.ldx, 1, 0, kBM) ||
+      if (!make_map(&a.a, p.type, p.x, p.k, p.rows, p.ldx, 1, 0, kBM) || !make_map(&a.few, p.type, p.x, p.k, p.rows, p.ldx, 1, 0, kFewRows) ||
           !make_map(&a.b, p.type, p.w, w_cols, w_rows, p.ldw, p.groups, p.stride_w, p.transposed ? bn : kBK))
         return cudaErrorNotSupported;
     }
