@@ -202,20 +202,25 @@ struct RowStore {
       }
     } else if (size == 4) {
       const int c = lane & 15;
-      for (int r = lane >> 4; r < min(32, rows_left); r += 2)
-        if (c0 + c < cols_left) reinterpret_cast<float*>(out)[r * ld + c0 + c] = reinterpret_cast<const float*>(unit(r, c >> 2))[c & 3];
+      float* at = reinterpret_cast<float*>(out) + (lane >> 4) * ld + c0 + c;
+#pragma unroll 4
+      for (int r = lane >> 4; r < 32; r += 2, at += 2 * ld)
+        if (r < rows_left && c0 + c < cols_left) *at = reinterpret_cast<const float*>(unit(r, c >> 2))[c & 3];
     } else {
       // word j of a row holds columns 2 j and 2 j + 1, or, where the row starts in the middle of a word, 2 j - 1 and 2 j: then the first and
       // the last column of the step go alone
       const int j = lane & 15, some = cols_left - c0;
-      const auto half = [&](int r, int c) { return (uint32_t)reinterpret_cast<const unsigned short*>(unit(r, c >> 3))[c & 7]; };
-      for (int r = lane >> 4; r < min(32, rows_left); r += 2) {
-        unsigned short* const row = reinterpret_cast<unsigned short*>(out) + r * ld + c0;
-        const int c = 2 * j - (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
-        if (c >= 0 && c + 1 < some) *reinterpret_cast<uint32_t*>(row + c) = half(r, c) | half(r, c + 1) << 16;
-        else if (c >= 0 && c < some) row[c] = (unsigned short)half(r, c);
-        else if (c < 0) row[0] = (unsigned short)half(r, 0);
-        if (j == 15 && c < 30 && 31 < some) row[31] = (unsigned short)half(r, 31);
+      unsigned short* row = reinterpret_cast<unsigned short*>(out) + (lane >> 4) * ld + c0;
+#pragma unroll 4
+      for (int r = lane >> 4; r < 32; r += 2, row += 2 * ld) {
+        const uint32_t word = reinterpret_cast<const uint32_t*>(unit(r, j >> 2))[j & 3], before = __shfl_up_sync(0xffffffffu, word, 1, 16);
+        const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0, there = r < rows_left;
+        const int c = odd ? 2 * j - 1 : 2 * j;
+        const uint32_t w = odd ? __byte_perm(before, word, 0x5432) : word;
+        if (there && c >= 0 && c + 1 < some) *reinterpret_cast<uint32_t*>(row + c) = w;
+        if (there && c >= 0 && c + 1 == some) row[c] = (unsigned short)w;
+        if (there && c < 0) row[0] = (unsigned short)word;
+        if (there && odd && j == 15 && 31 < some) row[31] = (unsigned short)(word >> 16);
       }
     }
     __syncwarp();
