@@ -381,39 +381,6 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   typename J::Item it;
   typename J::Walk walk = job.start(worker, workers);
 
-  // Issues the instructions of a chunk and what announces their end; by one thread.
-  const uint32_t kind = instruction<J::kAMn, J::kBMn, PAIR>(job.bf16());
-  const auto issue = [&](int slot, int set, int columns, int steps, bool first, bool ends) {
-    const uint32_t at = base + (uint32_t)slot * G::kStage, idesc = kind | (uint32_t)((PAIR ? BN : (min(columns, BN) + 15) / 16 * 16) >> 3) << 17;
-    const uint32_t a = desc_lo<J::kAMn>(at), b = desc_lo<J::kBMn>(at + PARTS * kATile);
-    constexpr uint32_t pa = kATile >> 4, pb = G::kBTile >> 4, oa = kStep16<J::kAMn>, ob = kStep16<J::kBMn>;
-    const uint32_t d = tmem + (uint32_t)(set * G::kAccs * BN);
-    for (int k = 0; k < steps; ++k) {
-      const uint32_t ak = a + k * oa, bk = b + k * ob, go_on = !first || k > 0;
-      if constexpr (PAIR) {
-        mma_pair(d, ak, bk, idesc, go_on);
-      } else {
-        mma(d, ak, bk, idesc, go_on);
-        if constexpr (PARTS > 1) {
-          mma(d + BN, ak, bk + pb, idesc, go_on);
-          mma(d + BN, ak + pa, bk, idesc, 1u);
-        }
-        if constexpr (PARTS > 2) {
-          mma(d + BN, ak + pa, bk + pb, idesc, 1u);
-          mma(d + BN, ak, bk + 2 * pb, idesc, 1u);
-          mma(d + BN, ak + 2 * pa, bk, idesc, 1u);
-        }
-      }
-    }
-    if constexpr (PAIR) {
-      commit_pair(empty + 8 * slot);
-      if (ends) commit_pair(acc_full + 8 * set);
-    } else {
-      gtc::mma_commit(empty + 8 * slot);
-      if (ends) gtc::mma_commit(acc_full + 8 * set);
-    }
-  };
-
   // Registers go where they are needed.  384 threads start with 168 each: the epilogue's eight warps get 208, the four others 80 (256 x 208 + 128 x 80 = 63488
   // of 64512).  640 threads start with 96: the epilogue gets 104, the eight loading warps 112 and the four others 48 (256 x 104 + 256 x 112 + 128 x 48 = 61440,
   // all there are).
@@ -466,25 +433,67 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       }
     }
   } else if (warp == kMmaWarp) {
-    int slot = 0, set = 0;
-    uint32_t parity = 0, acc_parity = 1;
-    bool ok = rank == 0;
-    while (ok && job.next(walk, it)) {
-      for (int c = 0; c < it.chunks; ++c) {
-        const bool first = (c & (segment - 1)) == 0, last = c + 1 == it.chunks, ends = last || (c & (segment - 1)) == segment - 1;
-        const bool clears = J::kTma && J::kAMn && last && it.tail < kBK;
-        ok = __all_sync(0xffffffffu, (!first || gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp)) &&
-                                         gtc::mbar_wait_abortable(full + 8 * slot, parity, abortp));
-        if (!ok) break;
-        if (PAIR && clears) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the other block's stores
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (lane == 0) issue(slot, set, it.n, clears ? (it.tail + 15) / 16 : kBK / 16, first, ends);
-        __syncwarp();
-        if (ends) {
-          if (set == 1) acc_parity ^= 1u;
-          set ^= 1;
+    // One thread waits and issues, with as little as possible between a chunk's last instruction and the next one's first: what the loop takes beyond the
+    // 512 clocks of a chunk's instructions (256 x 256 by a pair) is time that the tensor core stands still.  So what a chunk needs is kept in
+    // counters that are added to, and decisions are per segment.  (A chunk took 710 clocks with all of them made for every chunk.)
+    if (lane == 0 && rank == 0) {
+      const uint32_t kind = instruction<J::kAMn, J::kBMn, PAIR>(job.bf16());
+      constexpr uint32_t pa = kATile >> 4, pb = G::kBTile >> 4, oa = kStep16<J::kAMn>, ob = kStep16<J::kBMn>, kStride = G::kStage >> 4;
+      const uint32_t a0 = desc_lo<J::kAMn>(base), b_behind = desc_lo<J::kBMn>(base + PARTS * kATile) - a0;   // fields do not carry into each other
+      uint32_t a = a0, at = 0, parity = 0, set = 0, acc_parity = 1;   // descriptor of A, offset of the barriers
+      bool ok = true;
+      while (ok && job.next(walk, it)) {
+        const uint32_t idesc = kind | (uint32_t)((PAIR ? BN : (min(it.n, BN) + 15) / 16 * 16) >> 3) << 17;
+        const int chunks = it.chunks, tail_steps = J::kTma && J::kAMn ? (it.tail + 15) / 16 : kBK / 16;
+        for (int c = 0; c < chunks && ok;) {
+          const int stop = min(chunks, c + segment);
+          const uint32_t d = tmem + set * (G::kAccs * BN);
+          ok = gtc::mbar_wait_abortable(acc_empty + 8 * set, acc_parity, abortp);
+          if (!ok) break;
+          uint32_t go_on = 0;
+          for (; c < stop; ++c) {
+            ok = gtc::mbar_wait_abortable(full + at, parity, abortp);
+            if (!ok) break;
+            if (PAIR && J::kAMn && c + 1 == chunks) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // what the other block has cleared
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t b = a + b_behind;
+            const auto step = [&](int k, uint32_t more) {
+              const uint32_t ak = a + k * oa, bk = b + k * ob;
+              if constexpr (PAIR) {
+                mma_pair(d, ak, bk, idesc, more);
+              } else {
+                mma(d, ak, bk, idesc, more);
+                if constexpr (PARTS > 1) {
+                  mma(d + BN, ak, bk + pb, idesc, more);
+                  mma(d + BN, ak + pa, bk, idesc, 1u);
+                }
+                if constexpr (PARTS > 2) {
+                  mma(d + BN, ak + pa, bk + pb, idesc, 1u);
+                  mma(d + BN, ak, bk + 2 * pb, idesc, 1u);
+                  mma(d + BN, ak + 2 * pa, bk, idesc, 1u);
+                }
+              }
+            };
+            step(0, go_on);
+            if (J::kTma && J::kAMn && c + 1 == chunks) {
+              for (int k = 1; k < tail_steps; ++k) step(k, 1u);
+            } else {
+#pragma unroll
+              for (int k = 1; k < kBK / 16; ++k) step(k, 1u);
+            }
+            go_on = 1;
+            if constexpr (PAIR) commit_pair(empty + at);
+            else gtc::mma_commit(empty + at);
+            a += kStride;
+            at += 8;
+            if (at == 8 * S) { a = a0; at = 0; parity ^= 1u; }
+          }
+          if (!ok) break;
+          if constexpr (PAIR) commit_pair(acc_full + 8 * set);
+          else gtc::mma_commit(acc_full + 8 * set);
+          acc_parity ^= set;
+          set ^= 1u;
         }
-        if (++slot == S) { slot = 0; parity ^= 1u; }
       }
     }
   }
