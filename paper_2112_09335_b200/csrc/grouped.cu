@@ -91,7 +91,8 @@ struct ProductArgs {
   CUtensorMap a, b, few;   // of x and of the weights, where tiles are copied by TMA; of x in boxes of kFewRows rows
   Product p;
   int* error_flag;
-  bool vec_x, vec_w, vec_y;   // rows start on 16-byte boundaries
+  bool vec_x, vec_w;     // rows start on 16-byte boundaries
+  int boundary;          // of the rows of y
 };
 
 // The weights of a product of many rows, fp32, as the three parts of their elements: images of part 0 of all matrices, then part 1 and 2, rows padded to 16
@@ -124,7 +125,7 @@ struct ProductJob {
   using T = T_;
   using Args = ProductArgs;
   static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kTmaB = SPLIT, kMeets = false, kPair = PAIR;
+  static constexpr bool kAMn = false, kBMn = !TRANSPOSED, kTma = TMA, kTmaB = SPLIT, kTailed = false, kMeets = false, kPair = PAIR;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM;
   struct Item {
     int chunks, n, tail, g, row0, left, col0;
@@ -231,7 +232,7 @@ struct ProductJob {
     const int row = (warp & 3) * 32, col = (warp >> 2) * NC;
     const long long at = (it.row0 + row) * a.p.ldy + it.col0 + col;
     void* const y = a.p.out_type == kF32 ? (void*)(static_cast<float*>(a.p.y) + at) : (void*)(static_cast<unsigned short*>(a.p.y) + at);
-    store_rows<NC>(acc, buf, y, a.p.ldy, a.p.out_type, a.vec_y, it.left - row, it.n - col);
+    store_rows<NC>(acc, buf, y, a.p.ldy, a.p.out_type, a.boundary, it.left - row, it.n - col);
   }
 };
 
@@ -248,7 +249,8 @@ struct ProductTnArgs {
   CUtensorMap a, b;
   ProductTn p;
   int* error_flag;
-  bool vec_x, vec_y, vec_w;   // rows start on 16-byte boundaries
+  bool vec_x, vec_y;    // rows start on 16-byte boundaries
+  int boundary;         // of the rows of dw
   float* space;         // two tiles of sums for every block
   unsigned* tickets;    // three for every block
 };
@@ -262,7 +264,7 @@ struct ProductTnJob {
   using Args = ProductTnArgs;
   using Size = unsigned long long;
   static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kTmaB = false, kMeets = true, kPair = PAIR;
+  static constexpr bool kAMn = true, kBMn = true, kTma = TMA, kTmaB = false, kTailed = TMA, kMeets = true, kPair = PAIR;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kRanks = PAIR ? 2 : 1;
   struct Item {
     int chunks, n, tail, g, row0, end, m0, col0;
@@ -457,7 +459,7 @@ struct ProductTnJob {
     }
     const long long at = it.g * a.p.stride_dw + row * a.p.lddw + col;
     void* const dw = a.p.out_type == kF32 ? (void*)(static_cast<float*>(a.p.dw) + at) : (void*)(static_cast<unsigned short*>(a.p.dw) + at);
-    store_rows<NC>(acc, buf, dw, a.p.lddw, a.p.out_type, a.vec_w, a.p.ka - row, a.p.nb - col);
+    store_rows<NC>(acc, buf, dw, a.p.lddw, a.p.out_type, a.boundary, a.p.ka - row, a.p.nb - col);
   }
 };
 
@@ -468,12 +470,12 @@ struct ProductTnJob {
 //    O O + (D_i + D_j) O_ij), and X, a pair of halves, is itself multiplied by a + P_ii in fp32.  For results of bf16, whose
 //    rounding is 1.7e-3 of the result: five steps end 0.5 to 0.8e-3 off (1.3e-3 where 280 of 300 singular values are 1e-3 of the rest), in a third of the
 //    instructions.  With the diagonals inside it is 1.3 to 1.8e-3, with X in halves only 1e-3 to 4e-2: the steps lift small singular values, and what they are off, by |a| each.
-// Matrices between products are images: part hi of all matrices, then part lo, rows padded to 16 bytes, under a power of two that comes from
+// Matrices between products are images: part hi of all matrices, then part lo, rows padded to 32 bytes, under a power of two that comes from
 // the bounds of the singular values (host, grow()): entries stay below 2^15 and far above the smallest half.  S and P are symmetric: only
 // tiles that reach the diagonal are formed, the others are written turned.  X keeps its own orientation throughout, so nothing is transposed.
 struct Image {
   __half* at;
-  int rows, ld;            // ld: columns rounded up to 8
+  int rows, ld;            // ld: columns rounded up to 16, so that rows are whole sectors
   long long part;          // from hi to lo
   __device__ __forceinline__ __half* matrix(int b) const { return at + (long long)b * rows * ld; }
 };
@@ -686,14 +688,14 @@ struct OrthogonalArgs {
   void* out;                    // last kMove: the caller's matrix
   int out_type;
   long long ldo, stride_o;
-  bool vec_o;
+  int boundary;                 // of its rows
 };
 
 template <Stage STAGE, int PARTS, int BN, bool A_MN, bool B_MN, bool PAIR>
 struct OrthogonalJob {
   using Args = OrthogonalArgs;
   static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kTmaB = false, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
+  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kTmaB = false, kTailed = false, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
   static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kBCols = PAIR ? BN / 2 : BN;
   struct Item {
     int chunks, n, tail, matrix, row0, col0;
@@ -765,66 +767,41 @@ struct OrthogonalJob {
       }
     }
   }
-  // 32 rows x 32 columns of an image, from column c0 on, as they lie in memory: whole sectors, eight rows at a time.  On their way while the columns
-  // before are worked on, the first while the tile's products are formed: 16 of 1024 x 2048, this product WAS us where each
-  // was waited for, WITH us so.
+  // 32 elements of this lane's row of an image, two sectors of each part.  On their way while the columns before are worked on, the first while the
+  // tile's products are formed.
   static constexpr bool kReads = STAGE == kPolynomial || (STAGE == kMove && PARTS == 1);
   [[maybe_unused]] static constexpr bool kReadsLow = PARTS == 2 ? STAGE == kPolynomial : STAGE == kMove;
   struct Block {
-    uint4 hi[4], lo[kReadsLow ? 4 : 1];
+    uint32_t hi[16], lo[kReadsLow ? 16 : 1];
   };
   using Early = std::conditional_t<kReads, Block, Nothing>;
-  __device__ __forceinline__ void fetch(const Item& it, int row0, int col, Block& b) const {
-    const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
-    const __half* const at = a.s.matrix(it.matrix) + (long long)(row0 + r0) * a.s.ld + col + 8 * q;
+  __device__ __forceinline__ void fetch(const Item& it, int row, int col, Block& b) const {
+    const __half* const at = a.s.matrix(it.matrix) + (long long)row * a.s.ld + col;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = row0 + 8 * i + r0 < a.s.rows && col + 8 * q < a.s.ld;
-      b.hi[i] = there ? *reinterpret_cast<const uint4*>(at + (long long)8 * i * a.s.ld) : make_uint4(0u, 0u, 0u, 0u);
-      if (kReadsLow) b.lo[i] = there ? *reinterpret_cast<const uint4*>(at + (long long)8 * i * a.s.ld + a.s.part) : make_uint4(0u, 0u, 0u, 0u);
-    }
-  }
-  __device__ __forceinline__ void early(const Item& it, int warp, Early& b) const {
-    if constexpr (kReads) fetch(it, it.row0 + (warp & 3) * 32, it.col0 + (warp >> 2) * (BN / 2), b);
-  }
-  // This lane's row of such a block, as 16 words, through the buffer.
-  __device__ __forceinline__ static void hand_out(const RowStore& through, const uint4 (&b)[4], uint32_t (&w)[16]) {
-    const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
+    for (int h = 0; h < 2; ++h) {
+      if (row < a.s.rows && col + 16 * h < a.s.ld) {
+        load32(at + 16 * h, b.hi + 8 * h);
+        if constexpr (kReadsLow) load32(at + 16 * h + a.s.part, b.lo + 8 * h);
+      } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(through.unit(8 * i + r0, q)) = b[i];
-    __syncwarp();
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const uint4 v = *reinterpret_cast<const uint4*>(through.unit(lane, u));
-      w[4 * u] = v.x; w[4 * u + 1] = v.y; w[4 * u + 2] = v.z; w[4 * u + 3] = v.w;
-    }
-    __syncwarp();
-  }
-  __device__ __forceinline__ static float2 floats(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-  // 32 rows x 32 columns of halves, a row a lane, as 32 rows x 32 columns of the turned matrix at `out`.
-  __device__ __forceinline__ static void put_turned(const RowStore& through, const uint32_t (&w)[16], __half* out, long long ld, int rows_left, int cols_left) {
-    const int lane = threadIdx.x & 31, q = lane & 3;
-#pragma unroll
-    for (int c = 0; c < 32; ++c)
-      *reinterpret_cast<unsigned short*>(through.unit(c, lane >> 3) + (lane & 7) * 2) = (unsigned short)(w[c >> 1] >> (16 * (c & 1)));
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = 8 * i + (lane >> 2), some = rows_left - 8 * q;
-      __half* const at = out + c * ld + 8 * q;
-      if (c < cols_left && some > 0) {
-        const uint4 v = *reinterpret_cast<const uint4*>(through.unit(c, q));
-        if (some >= 8) {
-          *reinterpret_cast<uint4*>(at) = v;
-        } else {
-          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < some) reinterpret_cast<unsigned short*>(at)[e] = (unsigned short)(x[e >> 1] >> (16 * (e & 1)));
+        for (int e = 0; e < 8; ++e) {
+          b.hi[8 * h + e] = 0u;
+          if constexpr (kReadsLow) b.lo[8 * h + e] = 0u;
         }
       }
     }
-    __syncwarp();
+  }
+  __device__ __forceinline__ void early(const Item& it, int warp, Early& b) const {
+    if constexpr (kReads) fetch(it, it.row0 + (warp & 3) * 32 + (threadIdx.x & 31), it.col0 + (warp >> 2) * (BN / 2), b);
+  }
+  __device__ __forceinline__ static float2 floats(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+  // 32 rows x 32 columns of halves, a row a lane, as columns x rows of the turned matrix at `out`: 64 bytes of a row at once.
+  __device__ __forceinline__ static void put_turned(const uint32_t (&w)[16], __half* out, long long ld, int rows_left, int cols_left) {
+    const int lane = threadIdx.x & 31;
+    if (lane >= rows_left) return;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      if (c < cols_left) reinterpret_cast<unsigned short*>(out)[c * ld + lane] = (unsigned short)(w[c >> 1] >> (16 * (c & 1)));
   }
   // 32 columns at a time from sums to what is stored of them: few registers beside the sums
   template <int NC>
@@ -847,8 +824,8 @@ struct OrthogonalJob {
     const int out_size = a.out_type == kF32 ? 4 : 2;
     __half* const to = a.to.matrix(it.matrix);
     // images have room up to their leading dimension, and whole units there
-    const RowStore hi_to = out ? RowStore(buf, static_cast<uint8_t*>(a.out) + ((long long)it.matrix * a.stride_o + row0 * a.ldo + col0) * out_size, a.ldo, out_size, a.vec_o, rows_left, cols_left)
-                               : RowStore(buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, 2, true, rows_left, a.to.ld - col0);
+    const RowStore hi_to = out ? RowStore(buf, static_cast<uint8_t*>(a.out) + ((long long)it.matrix * a.stride_o + row0 * a.ldo + col0) * out_size, a.ldo, out_size, a.boundary, rows_left, cols_left)
+                               : RowStore(buf, to + (long long)row0 * a.to.ld + col0, a.to.ld, 2, 32, rows_left, a.to.ld - col0);
 #pragma unroll
     for (int c0 = 0; c0 < NC; c0 += 32) {
       if (c0 < cols_left) {
@@ -856,10 +833,8 @@ struct OrthogonalJob {
 #pragma unroll
         for (int c = 0; c < 32; ++c) x[c] = acc[c0 + c] * a.factor;
         if constexpr (kReads) {
-          uint32_t h[16], l[16];
-          hand_out(hi_to, next.hi, h);
-          if constexpr (kReadsLow) hand_out(hi_to, next.lo, l);
-          if (c0 + 32 < NC) fetch(it, row0, col0 + c0 + 32, next);
+          const Block now = next;
+          if (c0 + 32 < NC) fetch(it, row, col0 + c0 + 32, next);
           // of S b, with its diagonals apart b + c (D_i + D_j); of X the diagonal of P and a
           const auto weight = [&](int c) {
             if (STAGE == kPolynomial) return PARTS == 1 ? fmaf(a.factor, mine + __shfl_sync(0xffffffffu, theirs[c0 / 32], c), a.linear) : a.linear;
@@ -867,9 +842,9 @@ struct OrthogonalJob {
           };
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            float2 v = floats(h[e]);
+            float2 v = floats(now.hi[e]);
             if constexpr (kReadsLow) {
-              const float2 low = floats(l[e]);
+              const float2 low = floats(now.lo[e]);
               v = make_float2(fmaf(low.x, 0x1p-11f, v.x), fmaf(low.y, 0x1p-11f, v.y));
             }
             x[2 * e] = fmaf(weight(2 * e), v.x, x[2 * e]);
@@ -904,7 +879,7 @@ struct OrthogonalJob {
           hi_to.put(c0, make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7]), make_uint4(h[8], h[9], h[10], h[11]), make_uint4(h[12], h[13], h[14], h[15]));
           if (!out) {
             __half* const turned = to + (long long)(col0 + c0) * a.to.ld + row0;
-            if (it.turn) put_turned(hi_to, h, turned, a.to.ld, rows_left, cols_left - c0);
+            if (it.turn) put_turned(h, turned, a.to.ld, rows_left, cols_left - c0);
             if constexpr (PARTS == 2 || STAGE == kMove) {
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
@@ -914,7 +889,7 @@ struct OrthogonalJob {
               RowStore lo_to = hi_to;
               lo_to.out += 2 * a.to.part;
               lo_to.put(c0, make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7]), make_uint4(h[8], h[9], h[10], h[11]), make_uint4(h[12], h[13], h[14], h[15]));
-              if (it.turn) put_turned(hi_to, h, turned + a.to.part, a.to.ld, rows_left, cols_left - c0);
+              if (it.turn) put_turned(h, turned + a.to.part, a.to.ld, rows_left, cols_left - c0);
             }
           }
         }
@@ -944,6 +919,12 @@ bool fits_pairs(int n) { return cdiv(n, 256) * 256 * 4 <= 5LL * n; }
 
 // Whether every row of a matrix starts on a 16-byte boundary.
 bool even(const void* p, long long ld, int size) { return reinterpret_cast<std::uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0; }
+
+// Bytes, 32, 16 or 1, that every row of every matrix starts at a multiple of.
+int boundary_of(const void* p, long long ld, long long stride, int size) {
+  const unsigned long long low = reinterpret_cast<std::uintptr_t>(p) | (unsigned long long)ld * size | (unsigned long long)stride * size;
+  return low % 32 == 0 ? 32 : low % 16 == 0 ? 16 : 1;
+}
 
 // Tensor map of `depth` row-major matrices of 16-bit elements, rows x cols, for tiles of box_rows rows and 64 columns with the 128-byte swizzle;
 // elements outside of a matrix read as zero.  False where there is no such map (the operand then goes through registers).
@@ -1060,7 +1041,7 @@ struct OrthogonalSpace {
     };
     partial = static_cast<double*>(take((std::size_t)o.batch * kNormBlocks * sizeof(double)));
     const auto image = [&](int rows, int cols) {
-      const int ld = (cols + 7) / 8 * 8;
+      const int ld = (cols + 15) / 16 * 16;
       const long long part = (long long)o.batch * rows * ld;
       return Image{static_cast<__half*>(take(2 * part * sizeof(__half))), rows, ld, part};
     };
@@ -1095,7 +1076,7 @@ cudaError_t enqueue(const Product& p, const Room& room) {
   const int size = size_of(p.type);
   a.vec_x = even(p.x, p.ldx, size);
   a.vec_w = even(p.w, p.ldw, size) && (p.groups == 1 || p.stride_w * size % 16 == 0);
-  a.vec_y = even(p.y, p.ldy, size_of(p.out_type));
+  a.boundary = boundary_of(p.y, p.ldy, 0, size_of(p.out_type));
   const long long tiles_m = std::min<long long>(p.rows, cdiv(p.rows, kBM) + p.groups);   // at most, wherever the groups begin
   if (p.type != kF32 && a.vec_x && a.vec_w && fits_pairs(p.n) && std::min<long long>(p.rows, cdiv(p.rows, 2 * kBM) + p.groups) * cdiv(p.n, 256) >= kSms / 2) {
     const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
@@ -1153,7 +1134,7 @@ cudaError_t enqueue(const ProductTn& p, const Room& room) {
   const int size = size_of(p.type);
   a.vec_x = even(p.x, p.ldx, size);
   a.vec_y = even(p.y, p.ldy, size);
-  a.vec_w = even(p.dw, p.lddw, size_of(p.out_type)) && (p.groups == 1 || p.stride_dw * size_of(p.out_type) % 16 == 0);
+  a.boundary = boundary_of(p.dw, p.lddw, p.groups > 1 ? p.stride_dw : 0, size_of(p.out_type));
   const TnPlan t = plan(p);
   a.space = static_cast<float*>(room.space);
   a.tickets = room.tickets;
@@ -1268,7 +1249,7 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
       move.out_type = p.out_type;
       move.ldo = p.ldo;
       move.stride_o = p.stride_o;
-      move.vec_o = even(p.out, p.ldo, size_of(p.out_type)) && (p.batch == 1 || p.stride_o * size_of(p.out_type) % 16 == 0);
+      move.boundary = boundary_of(p.out, p.ldo, p.batch > 1 ? p.stride_o : 0, size_of(p.out_type));
     }
     const auto step = [&](auto parts, auto width) {
       constexpr int PARTS = decltype(parts)::value, BN = decltype(width)::value;

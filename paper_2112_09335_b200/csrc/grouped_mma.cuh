@@ -118,6 +118,14 @@ __device__ __forceinline__ void arrive_at_first(uint32_t there, bool wrote) {
     else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(there) : "memory");
   }
 }
+// Of a phase that is known to be over: what the other block stored before it arrived is seen.
+__device__ __forceinline__ void acquire_cluster(uint32_t bar, uint32_t parity) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}"
+      ::"r"(bar), "r"(parity)
+      : "memory");
+}
 // Announces `bytes` at `bar` and arrives there; where THERE, the first block's.
 template <bool THERE>
 __device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
@@ -155,10 +163,20 @@ struct Bars {
   uint64_t full[8], empty[8], acc_full[2], acc_empty[2], tail[8], drain;
 };
 
-// NC columns of 32 rows, one row a lane, to `out` (element (0, 0) of the warp's part), the first rows_left rows and cols_left columns of them.
-// Through a buffer, so that what leaves a warp at once are 64 bytes of each of eight rows, whole sectors.  vec: rows of `out` start on
-// 16-byte boundaries; where they do not, or end inside of 16 bytes, a warp writes 32 columns of a row (fp32) or of two rows at once, halves two by two in whichever way they are
-// aligned (13752 x 767 halves, with its product: 87 us where each lane wrote eight halves one by one, 69 us so).
+// Rows of what a warp leaves, one row a lane, 64 bytes of each at a time.  Where rows lie on 32-byte boundaries every lane writes whole sectors of its own row, at
+// once.  Otherwise they go through a buffer in shared memory, so that what leaves a warp at once are 64 bytes of each of eight rows; where they
+// do not lie on 16-byte boundaries either, or end inside of 16 bytes, a warp writes 16 columns (fp32) or 32 of two rows at once, halves two by
+// two in whichever way they are aligned (13752 x 767 halves, with their product: 87 us where each lane wrote eight halves one by one, 42 us
+// so).  The buffer is not for all: while a pair multiplies, its operands alone take 128 bytes a clock from and to shared memory, all there are.
+__device__ __forceinline__ void store32(void* at, const uint4& a, const uint4& b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+__device__ __forceinline__ void load32(const void* at, uint32_t* w) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(at)
+               : "memory");
+}
 __device__ __forceinline__ uint32_t pack(int type, float x, float y) {
   if (type == kBf16) {
     const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
@@ -175,14 +193,21 @@ struct RowStore {
   uint8_t* out;
   long long ld;
   int size, rows_left, cols_left;   // size: bytes of an element
-  bool whole, units;                // all rows there; rows of whole units of 16 bytes
-  __device__ __forceinline__ RowStore(uint8_t* buf_, void* out_, long long ld_, int size_, bool vec, int rows_left_, int cols_left_)
-      : buf(buf_), out(static_cast<uint8_t*>(out_)), ld(ld_), size(size_), rows_left(rows_left_), cols_left(cols_left_), whole(vec && rows_left_ >= 32),
-        units(vec && (cols_left_ * size_ & 15) == 0) {}
+  bool direct, units;               // rows of whole sectors of 32 bytes, of whole units of 16
+  // boundary: bytes that every row starts at a multiple of, 32, 16 or less
+  __device__ __forceinline__ RowStore(uint8_t* buf_, void* out_, long long ld_, int size_, int boundary, int rows_left_, int cols_left_)
+      : buf(buf_), out(static_cast<uint8_t*>(out_)), ld(ld_), size(size_), rows_left(rows_left_), cols_left(cols_left_),
+        direct(boundary >= 32 && (cols_left_ * size_ & 31) == 0), units(boundary >= 16 && (cols_left_ * size_ & 15) == 0) {}
   __device__ __forceinline__ uint8_t* unit(int r, int u) const { return buf + r * 64 + ((u ^ ((r >> 1) & 3)) << 4); }
   // 64 bytes of this lane's row, from column c0 on.
   __device__ __forceinline__ void put(int c0, const uint4& w0, const uint4& w1, const uint4& w2, const uint4& w3) const {
     const int lane = threadIdx.x & 31, q = lane & 3, r0 = lane >> 2;
+    if (direct) {
+      uint8_t* const at = out + (lane * ld + c0) * size;
+      if (lane < rows_left) store32(at, w0, w1);
+      if (lane < rows_left && c0 * size + 32 < cols_left * size) store32(at + 32, w2, w3);
+      return;
+    }
     *reinterpret_cast<uint4*>(unit(lane, 0)) = w0;
     *reinterpret_cast<uint4*>(unit(lane, 1)) = w1;
     *reinterpret_cast<uint4*>(unit(lane, 2)) = w2;
@@ -192,14 +217,9 @@ struct RowStore {
     if (units) {
       uint8_t* const at = out + (r0 * ld + c0) * size + 16 * q;
       const long long down = 8 * ld * size;
-      if (whole && (cols_left - c0) * size >= 64) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (8 * i + r0 < rows_left && c0 * size + 16 * q < cols_left * size) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
-      }
+      for (int i = 0; i < 4; ++i)
+        if (8 * i + r0 < rows_left && c0 * size + 16 * q < cols_left * size) *reinterpret_cast<uint4*>(at + i * down) = *reinterpret_cast<const uint4*>(from + 512 * i);
     } else if (size == 4) {
       const int c = lane & 15;
       float* at = reinterpret_cast<float*>(out) + (lane >> 4) * ld + c0 + c;
@@ -227,8 +247,8 @@ struct RowStore {
   }
 };
 template <int NC>
-__device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf, void* out, long long ld, int out_type, bool vec, int rows_left, int cols_left) {
-  const RowStore to(buf, out, ld, out_type == kF32 ? 4 : 2, vec, rows_left, cols_left);
+__device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf, void* out, long long ld, int out_type, int boundary, int rows_left, int cols_left) {
+  const RowStore to(buf, out, ld, out_type == kF32 ? 4 : 2, boundary, rows_left, cols_left);
   if (out_type == kF32) {
 #pragma unroll
     for (int c0 = 0; c0 < NC; c0 += 16) {
@@ -307,7 +327,7 @@ struct Raw<unsigned short> {
 };
 
 // The shared loop.  A job J says what the items are, where operand tiles come from and what becomes of a tile's sums:
-//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kTmaB (of operands that go through registers B still comes by TMA), kPair, kMeets (finish() has barriers of the epilogue warps)
+//   J::Args, kParts, kBN, kAMn, kBMn, kTma, kTmaB (of operands that go through registers B still comes by TMA), kPair, kTailed (copies bring rows from behind the end of an item), kMeets (finish() has barriers of the epilogue warps)
 //   segment()                         chunks of a segment, a power of two
 //   J(args, tables, rank)             built by every thread (rank: of the block in its pair); setup(): tables in shared memory, by the whole
 //                                     block, between barriers
@@ -388,7 +408,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   if constexpr (J::kTma) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
   if (warp == kMmaWarp + 2 && J::kTma) {
-    if constexpr (J::kTma && J::kAMn) {
+    if constexpr (J::kTailed) {
       // Rows of the next group come with the last chunk of a tile: the steps that are still read are cleared in both operands, in a pair by each
       // block in its own.  A warp of its own does it while chunks before this one are multiplied, and then arrives where
       // copies of other chunks arrive.  (Where the issuing warp did it, chunks behind waited.)
@@ -424,7 +444,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
             const uint32_t tile = base + (uint32_t)slot * G::kStage;
             if constexpr (J::kTmaB) job.copy_b(it, c, tile + PARTS * kATile, full + 8 * slot);
             // a chunk with rows to clear is announced to the warp that does it
-            else if (J::kAMn && it.tail < kBK && c + 1 == it.chunks) job.template copy<false>(it, c, tile, tail + 8 * slot);
+            else if (J::kTailed && it.tail < kBK && c + 1 == it.chunks) job.template copy<false>(it, c, tile, tail + 8 * slot);
             else job.template copy<PAIR>(it, c, tile, full_there + 8 * slot);
             ++copies;
             if (++slot == S) { slot = 0; parity ^= 1u; }
@@ -444,7 +464,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       bool ok = true;
       while (ok && job.next(walk, it)) {
         const uint32_t idesc = kind | (uint32_t)((PAIR ? BN : (min(it.n, BN) + 15) / 16 * 16) >> 3) << 17;
-        const int chunks = it.chunks, tail_steps = J::kTma && J::kAMn ? (it.tail + 15) / 16 : kBK / 16;
+        const int chunks = it.chunks, tail_steps = J::kTailed ? (it.tail + 15) / 16 : kBK / 16;
         for (int c = 0; c < chunks && ok;) {
           const int stop = min(chunks, c + segment);
           const uint32_t d = tmem + set * (G::kAccs * BN);
@@ -454,7 +474,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
           for (; c < stop; ++c) {
             ok = gtc::mbar_wait_abortable(full + at, parity, abortp);
             if (!ok) break;
-            if (PAIR && J::kAMn && c + 1 == chunks) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // what the other block has cleared
+            if (PAIR && J::kTailed && c + 1 == chunks) acquire_cluster(full + at, parity);   // what the other block has cleared
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t b = a + b_behind;
             const auto step = [&](int k, uint32_t more) {
@@ -475,7 +495,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
               }
             };
             step(0, go_on);
-            if (J::kTma && J::kAMn && c + 1 == chunks) {
+            if (J::kTailed && c + 1 == chunks) {
               for (int k = 1; k < tail_steps; ++k) step(k, 1u);
             } else {
 #pragma unroll
