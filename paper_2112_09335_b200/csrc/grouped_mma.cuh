@@ -54,6 +54,7 @@ struct Geometry {
   static constexpr uint32_t kTmemCols = 2 * kAccs * BN;
   static constexpr int kBuffersAt = kStages * kStage, kTablesAt = kBuffersAt + kEpiWarps * kBuffer;
   static_assert(kTmemCols >= 32 && kTmemCols <= 512, "tensor memory");
+  static_assert(PARTS == 1 || 2 * BN <= 256, "columns of an instruction");
   static_assert(!PAIR || (PARTS == 1 && TMA && BN == 256), "the pair has one layout");
 };
 
@@ -464,6 +465,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
       bool ok = true;
       while (ok && job.next(walk, it)) {
         const uint32_t idesc = kind | (uint32_t)((PAIR ? BN : (min(it.n, BN) + 15) / 16 * 16) >> 3) << 17;
+        [[maybe_unused]] const uint32_t both = kind | (uint32_t)(2 * BN >> 3) << 17;
         const int chunks = it.chunks, tail_steps = J::kTailed ? (it.tail + 15) / 16 : kBK / 16;
         for (int c = 0; c < chunks && ok;) {
           const int stop = min(chunks, c + segment);
@@ -482,11 +484,10 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
               if constexpr (PAIR) {
                 mma_pair(d, ak, bk, idesc, more);
               } else {
-                mma(d, ak, bk, idesc, more);
-                if constexpr (PARTS > 1) {
-                  mma(d + BN, ak, bk + pb, idesc, more);
-                  mma(d + BN, ak + pa, bk, idesc, 1u);
-                }
+                // Part 0 of A with parts 0 and 1 of B, which lie one behind the other as do main sums and corrections: one instruction of 2 BN
+                // columns, which reads A once
+                mma(d, ak, bk, PARTS > 1 ? both : idesc, more);
+                if constexpr (PARTS > 1) mma(d + BN, ak + pa, bk, idesc, 1u);
                 if constexpr (PARTS > 2) {
                   mma(d + BN, ak + pa, bk + pb, idesc, 1u);
                   mma(d + BN, ak, bk + 2 * pb, idesc, 1u);
