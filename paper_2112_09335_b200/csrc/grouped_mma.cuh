@@ -168,12 +168,13 @@ struct Bars {
 // once.  Otherwise they go through a buffer in shared memory, so that what leaves a warp at once are 64 bytes of each of eight rows; where they
 // do not lie on 16-byte boundaries either, or end inside of 16 bytes, a warp writes 16 columns (fp32) or 32 of two rows at once, halves two by
 // two in whichever way they are aligned (13752 x 767 halves, with their product: 87 us where each lane wrote eight halves one by one, 42 us
-// so).  The buffer is not for all: while a pair multiplies, its operands alone take 128 bytes a clock from and to shared memory, all there are.
+// so).  Neither
+// is kept in L1 (169343 x 128 x 256 fp32 103 -> 92 us, 4096 x 4096 updates 1.44 -> 1.28 ms).  The buffer is not for all: while a pair multiplies, its operands alone take 128 bytes a clock from and to shared memory, all there are.
 __device__ __forceinline__ void store32(void* at, const uint4& a, const uint4& b) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+  asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 __device__ __forceinline__ void load32(const void* at, uint32_t* w) {
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
                : "l"(at)
                : "memory");
@@ -280,6 +281,11 @@ __device__ __forceinline__ void store_rows(const float (&acc)[NC], uint8_t* buf,
 // Eight elements of a row on their way from memory to an operand tile, those from `valid` on zero.
 template <typename T>
 struct Raw;
+__device__ __forceinline__ float4 load16(const float* at) {   // read once by this SM
+  float4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(at));
+  return v;
+}
 template <>
 struct Raw<float> {
   float x[8];
@@ -288,8 +294,8 @@ struct Raw<float> {
   __device__ __forceinline__ void load(const float* p, int valid) {
     if constexpr (VEC) {
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-      if (valid > 0) a = __ldg(reinterpret_cast<const float4*>(p));
-      if (valid > 4) b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+      if (valid > 0) a = load16(p);
+      if (valid > 4) b = load16(p + 4);
       x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     } else {
 #pragma unroll
