@@ -195,9 +195,9 @@ int gcn_admm_dense_product_tn(gcn_admm* h, const float* A, const float* B, float
  * handle's communities, in the order of gcn_admm_index (n_groups and rows must then be the handle's).  Groups should not overlap (rows of two
  * groups get one of the two results).  Results may not alias operands.
  * All work is enqueued on the handle's stream; the calls return without synchronising, may be captured, and give the same bits
- * every time.  gcn_admm_grouped_product_tn and gcn_admm_orthogonalise use a workspace of the handle that grows when a call needs more
- * of it: the first call of a size allocates and may not be part of a capture.  Calls, and replays of captured ones, that share a handle must
- * follow one another on its stream.  A bounded wait that runs out on the device is reported like that of any product (see
+ * every time.  gcn_admm_grouped_product (fp32, many rows: its weights as three parts), gcn_admm_grouped_product_tn and
+ * gcn_admm_orthogonalise use a workspace of the handle that grows when a call needs more of it: the first call of a size allocates and may not be
+ * part of a capture (it is refused there).  Calls, and replays of captured ones, that share a handle must follow one another on its stream.  A bounded wait that runs out on the device is reported like that of any product (see
  * GCN_ADMM_ST_PIPELINE_FLAG). */
 enum { GCN_ADMM_F32 = 0, GCN_ADMM_BF16 = 1, GCN_ADMM_F16 = 2 };
 
@@ -218,8 +218,10 @@ int gcn_admm_grouped_product_tn(gcn_admm* h, int type, const void* x, long long 
  * `batch` matrices G, rows x cols, X_0 = G / (||G||_F + eps) and n_steps times X <- a X + (b A + c A A) X with A = X X^T (X^T in place
  * of X where rows > cols); out = scale X.  coefficients: a, b, c of every step, host array of 3 n_steps floats.  Each singular value s
  * goes to s (a + b s^2 + c s^4); coefficients that let one grow above 16, or a factor a + b s^2 + c s^4 above 1024, are refused.  A
- * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  All products to fp32 accuracy, whatever the type, by pairs of
- * halves under fixed scales (the entries are bounded by the singular values).  out may be g itself. */
+ * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  Results of fp32 and fp16 come from products to fp32 accuracy, by
+ * pairs of halves under fixed scales (the entries are bounded by the singular values); results of bf16 from products of single halves with the
+ * diagonals of A and of the polynomial, and a X, kept apart in fp32: 0.5 to 1.3e-3 of the result, beside 1.7e-3 of its rounding.  out may be g itself,
+ * with the same type and strides. */
 int gcn_admm_orthogonalise(gcn_admm* h, int type, int batch, int rows, int cols, const void* g, long long ldg, long long stride_g,
                            int n_steps, const float* coefficients, float eps, float scale, int out_type, void* out, long long ldo,
                            long long stride_o);

@@ -218,7 +218,7 @@ struct gcn_admm {
   int* d_comm_ptr = nullptr;              // [M+1] rows of the communities: the groups of a grouped product that names none
   gcn_admm_mem::Slab work;                // workspace of the grouped products and orthogonalised updates, counters of finished tiles first
   size_t work_tickets = 0;                // how many
-  std::vector<gcn_admm_mem::Slab> old_work;   // what it was before it grew: graphs that the caller captured still use it
+  std::vector<std::pair<gcn_admm_mem::Slab, size_t>> old_work;   // what it was before it grew, and its counters: graphs that the caller captured still use it
   unsigned char* d_train = nullptr;
   int* d_train_rows = nullptr;            // new ids of the training rows, ascending
   float* d_fista_momentum = nullptr;      // (t_j - 1) / t_{j+1}, j = 1..fista_iters
@@ -402,12 +402,22 @@ struct gcn_admm {
       const size_t count = std::max(tickets, work_tickets);
       old_work.reserve(old_work.size() + 1);
       gcn_admm_mem::Slab larger = take_slab(behind(count) + std::max(bytes, work.size - std::min(work.size, behind(work_tickets))));
-      if (work.base) old_work.push_back(work);
+      if (work.base) old_work.push_back({work, work_tickets});
       work = larger;
       work_tickets = count;
       CU(cudaMemsetAsync(work.base, 0, behind(count), stream));
     }
     return Room{work.base + behind(work_tickets), reinterpret_cast<unsigned*>(work.base), tc_error, stream, &launches};
+  }
+  // Runs one of the calls below, counted and, when profiling, timed under `name`.
+  template <typename F>
+  void book(const char* name, double bytes, double flops, const F& enqueue) {
+    const long long before = launches;
+    {
+      Scope sc(this, name, 0, bytes, flops);
+      CU(enqueue());
+    }
+    if (profiling) prof[name].launches += launches - before;
   }
   // Refuses pointers that kernels on this handle's device cannot follow.
   void need_device(std::initializer_list<const void*> pointers) const {
@@ -1130,6 +1140,8 @@ struct gcn_admm {
       CU(cudaMemsetAsync(&report->status, 0, sizeof(int), stream));   // decisions since then may have read anything
       for (const auto& c : counters) CU(cudaMemsetAsync(*c.first, 0, c.second, stream));
       if (work_tickets > 0) CU(cudaMemsetAsync(work.base, 0, work_tickets * sizeof(unsigned), stream));
+      for (const auto& q : old_work)
+        if (q.second > 0) CU(cudaMemsetAsync(q.first.base, 0, q.second * sizeof(unsigned), stream));
       fresh = false;
       throw Fail{GCN_ADMM_ERR_CUDA, r.error & gk::kErrGridBarrier ? "a step-size search gave up waiting for the rest of its grid"
                                                                   : "a tensor-core product gave up waiting on its pipeline"};
@@ -1645,7 +1657,7 @@ void gcn_admm_destroy(gcn_admm* h) {
       if (e) cudaEventDestroy(e);
     for (cudaEvent_t e : h->event_pool) cudaEventDestroy(e);
     for (const gcn_admm_mem::Slab& q : {h->slab, h->wide_sums, h->work}) gcn_admm_mem::Pool::get().give(q);
-    for (const gcn_admm_mem::Slab& q : h->old_work) gcn_admm_mem::Pool::get().give(q);
+    for (const auto& q : h->old_work) gcn_admm_mem::Pool::get().give(q.first);
     h->stage.close();
   }
   cudaGetLastError();
@@ -1951,8 +1963,7 @@ int gcn_admm_grouped_product(gcn_admm* h, int type, const void* x, long long ldx
     char name[48];
     std::snprintf(name, sizeof name, "grouped@%dx%d", k, n);
     const int size = gcn_admm_grouped::size_of(type);
-    gcn_admm::Scope sc(h, name, 0, (double)rows * k * size + (double)n_groups * k * n * size + (double)rows * n * gcn_admm_grouped::size_of(out_type), 2.0 * (double)rows * k * n);
-    CU(gcn_admm_grouped::enqueue(p, room));
+    h->book(name, (double)rows * k * size + (double)n_groups * k * n * size + (double)rows * n * gcn_admm_grouped::size_of(out_type), 2.0 * (double)rows * k * n, [&] { return gcn_admm_grouped::enqueue(p, room); });
   });
 }
 
@@ -1966,9 +1977,8 @@ int gcn_admm_grouped_product_tn(gcn_admm* h, int type, const void* x, long long 
     const gcn_admm_grouped::Room room = h->room_for(gcn_admm_grouped::space_bytes(p), gcn_admm_grouped::tickets_of(p));
     char name[48];
     std::snprintf(name, sizeof name, "grouped_tn@%dx%d", ka, nb);
-    gcn_admm::Scope sc(h, name, 0, (double)rows * (ka + nb) * gcn_admm_grouped::size_of(type) + (double)n_groups * ka * nb * gcn_admm_grouped::size_of(out_type),
-                       2.0 * (double)rows * ka * nb);
-    CU(gcn_admm_grouped::enqueue(p, room));
+    h->book(name, (double)rows * (ka + nb) * gcn_admm_grouped::size_of(type) + (double)n_groups * ka * nb * gcn_admm_grouped::size_of(out_type),
+                       2.0 * (double)rows * ka * nb, [&] { return gcn_admm_grouped::enqueue(p, room); });
   });
 }
 
@@ -1982,9 +1992,8 @@ int gcn_admm_orthogonalise(gcn_admm* h, int type, int batch, int rows, int cols,
     char name[48];
     std::snprintf(name, sizeof name, "orthogonalise@%dx%d", rows, cols);
     const double m = std::min(rows, cols), w = std::max(rows, cols);
-    gcn_admm::Scope sc(h, name, 0, (double)batch * m * w * (gcn_admm_grouped::size_of(type) + gcn_admm_grouped::size_of(out_type)),
-                       (double)batch * n_steps * (m * (m + 1) * w + m * (m + 1) * m + 2 * m * m * w));
-    CU(gcn_admm_grouped::enqueue(p, room));
+    h->book(name, (double)batch * m * w * (gcn_admm_grouped::size_of(type) + gcn_admm_grouped::size_of(out_type)),
+                       (double)batch * n_steps * (m * (m + 1) * w + m * (m + 1) * m + 2 * m * m * w), [&] { return gcn_admm_grouped::enqueue(p, room); });
   });
 }
 

@@ -483,7 +483,7 @@ struct Image {
 constexpr int kNormBlocks = 256;   // partial sums of a norm, at most
 
 // Partial sums of squares of every matrix; in fp64: squares of fp32 numbers leave the range of fp32.  (One load a thread and 64 blocks took 520 us
-// of 4096 x 4096 halves, eight elements a load and as many blocks as there is work for WITH.)
+// of 4096 x 4096 halves, eight elements a load and as many blocks as there is work for 24.)
 template <typename T>
 __global__ void __launch_bounds__(256) k_norm(const Orthogonal p, bool vec, double* __restrict__ partial) {
   gtc::enter_kernel();
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, con
 }
 
 // Matrices whose shorter side is at most 32, all steps in one launch: a block has a matrix in its shared memory, in fp32 and with fp32 FMA.  (Through the tensor cores
-// every step is three launches of tiles that are nearly empty: eight matrices of 128 x 16 took 73 us, WITH us so.)
+// every step is three launches of tiles that are nearly empty: eight matrices of 128 x 16 took 73 us, 16 us so.)
 // X lies as [n][M], its shorter side, padded to M, contiguous.  S: every warp adds up the products of its part of the n steps, a lane the M / 8 x M / 4
 // entries at its place, and the warps' sums are added in order.  X <- P X: a thread has columns of its own and reads P, the same for all.
 struct SmallSteps {
@@ -770,9 +770,9 @@ struct OrthogonalJob {
   // 32 elements of this lane's row of an image, two sectors of each part.  On their way while the columns before are worked on, the first while the
   // tile's products are formed.
   static constexpr bool kReads = STAGE == kPolynomial || (STAGE == kMove && PARTS == 1);
-  [[maybe_unused]] static constexpr bool kReadsLow = PARTS == 2 ? STAGE == kPolynomial : STAGE == kMove;
+  __host__ __device__ static constexpr bool reads_low() { return PARTS == 2 ? STAGE == kPolynomial : STAGE == kMove; }
   struct Block {
-    uint32_t hi[16], lo[kReadsLow ? 16 : 1];
+    uint32_t hi[16], lo[reads_low() ? 16 : 1];
   };
   using Early = std::conditional_t<kReads, Block, Nothing>;
   __device__ __forceinline__ void fetch(const Item& it, int row, int col, Block& b) const {
@@ -781,12 +781,12 @@ struct OrthogonalJob {
     for (int h = 0; h < 2; ++h) {
       if (row < a.s.rows && col + 16 * h < a.s.ld) {
         load32(at + 16 * h, b.hi + 8 * h);
-        if constexpr (kReadsLow) load32(at + 16 * h + a.s.part, b.lo + 8 * h);
+        if constexpr (reads_low()) load32(at + 16 * h + a.s.part, b.lo + 8 * h);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           b.hi[8 * h + e] = 0u;
-          if constexpr (kReadsLow) b.lo[8 * h + e] = 0u;
+          if constexpr (reads_low()) b.lo[8 * h + e] = 0u;
         }
       }
     }
@@ -843,7 +843,7 @@ struct OrthogonalJob {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float2 v = floats(now.hi[e]);
-            if constexpr (kReadsLow) {
+            if constexpr (reads_low()) {
               const float2 low = floats(now.lo[e]);
               v = make_float2(fmaf(low.x, 0x1p-11f, v.x), fmaf(low.y, 0x1p-11f, v.y));
             }
@@ -1057,7 +1057,7 @@ struct OrthogonalSpace {
 bool is_small(const Orthogonal& p);
 std::size_t space_bytes(const Orthogonal& p) { return is_small(p) ? 0 : OrthogonalSpace(p, nullptr).bytes; }
 
-// Whether the weights are split beforehand: where there are at least two tiles of rows to a group they are read again for every one (WITH).
+// Whether the weights are split beforehand: where there are at least two tiles of rows to a group they would be split again for every one.
 bool splits_weights(const Product& p) {
   const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
   return p.type == kF32 && p.rows >= 2LL * kBM * p.groups && w_rows * cdiv(w_cols, 8) < INT_MAX && gcn_admm_host::encode_tiled() != nullptr;
@@ -1087,7 +1087,7 @@ cudaError_t enqueue(const Product& p, const Room& room) {
   const bool x_quads = a.vec_x && p.k % 4 == 0, quads = x_quads && a.vec_w && (p.transposed || p.n % 4 == 0);   // rows of the operands are whole quads
   const auto pick = [&](auto tma) {
     // A tile costs its columns, and its 128 rows as much as 64 columns; what counts are the tiles that one SM has.  (Eight rows of 64 groups, 1024 x 2048: 256 tiles of
-    // 64 columns, two for some SMs, WAS us, 128 of 128 columns WITH.)
+    // 64 columns, two for some SMs, 18 us, 128 of 128 columns 11.)
     const auto cost = [&](int bn) { return cdiv(tiles_m * cdiv(p.n, bn), kSms) * (std::min(bn, p.n) + 64); };
     int bn = cost(128) <= cost(64) ? 128 : 64;
     if (decltype(tma)::value && cost(256) <= cost(bn)) bn = 256;

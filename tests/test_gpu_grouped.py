@@ -562,6 +562,80 @@ def test_captured_calls_replay_on_new_data():
         g.destroy()
 
 
+def test_calls_are_counted_and_timed(h):
+    import torch
+    x, w, y, off = torch.randn(40, 24, device="cuda"), torch.randn(2, 24, 16, device="cuda"), torch.empty(40, 16, device="cuda"), offsets_of([25, 15])
+    dw = torch.empty_like(w)
+
+    def calls():
+        h.grouped_product(x.data_ptr(), w.data_ptr(), y.data_ptr(), off.data_ptr(), 2, 40, 24, 16)
+        h.grouped_product_tn(x.data_ptr(), y.data_ptr(), dw.data_ptr(), off.data_ptr(), 2, 40, 24, 16)
+        h.orthogonalise(dw.data_ptr(), dw.data_ptr(), 2, 24, 16, [MUON] * 5)
+    calls()
+    before = h.launches()
+    h.profile(True)
+    calls()
+    got = h.profile_read()
+    h.profile(False)
+    for name in ("grouped@24x16", "grouped_tn@24x16", "orthogonalise@24x16"):
+        assert got[name]["launches"] >= 1 and got[name]["ms"] > 0 and got[name]["flops"] > 0, got
+    assert h.launches() - before == sum(v["launches"] for v in got.values())
+
+
+def test_a_first_call_may_be_captured():
+    """Where no workspace is needed nothing has to have run before."""
+    import torch
+    s = torch.cuda.Stream()
+    g = trainer(stream=s.cuda_stream)
+    try:
+        with torch.cuda.stream(s):
+            x, w = torch.randn(300, 72, device="cuda").half(), torch.randn(2, 72, 40, device="cuda").half()
+            y, off = torch.zeros(300, 40, device="cuda"), offsets_of([100, 200])
+            s.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s, capture_error_mode="thread_local"):
+                g.grouped_product(x.data_ptr(), w.data_ptr(), y.data_ptr(), off.data_ptr(), 2, 300, 72, 40, type=binding.F16, out_type=binding.F32)
+            graph.replay()
+            s.synchronize()
+        for i, (lo, hi) in enumerate(((0, 100), (100, 300))):
+            a, b = x[lo:hi].double(), w[i].double()
+            close(y[lo:hi], a @ b, a.abs() @ b.abs(), 72)
+        del graph
+    finally:
+        s.synchronize()
+        g.destroy()
+
+
+def test_two_handles_at_once():
+    """Handles on streams of their own share nothing: the same calls side by side give what they give alone."""
+    import torch
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    made = [trainer(stream=s.cuda_stream) for s in streams]
+    try:
+        x, w = torch.randn(5000, 200, device="cuda"), torch.randn(3, 200, 264, device="cuda")
+        off = offsets_of([2000, 2900, 100])
+        results = []
+        torch.cuda.synchronize()
+        for _ in range(3):
+            outs = []
+            for g in made:
+                y, dw, o = torch.empty(5000, 264, device="cuda"), torch.empty(3, 200, 264, device="cuda"), torch.empty(3, 200, 264, device="cuda")
+                torch.cuda.synchronize()
+                outs.append((y, dw, o))
+            for g, (y, dw, o) in zip(made, outs):
+                g.grouped_product(x.data_ptr(), w.data_ptr(), y.data_ptr(), off.data_ptr(), 3, 5000, 200, 264)
+                g.grouped_product_tn(x.data_ptr(), y.data_ptr(), dw.data_ptr(), off.data_ptr(), 3, 5000, 200, 264)
+                g.orthogonalise(dw.data_ptr(), o.data_ptr(), 3, 200, 264, [MUON] * 5)
+            torch.cuda.synchronize()
+            results += outs
+        for other in results[1:]:
+            for p, q in zip(results[0], other):
+                assert torch.equal(p, q)
+    finally:
+        for g in made:
+            g.destroy()
+
+
 # ---- used together ----------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("kind, out", [("f32", "f32"), ("bf16", "f32"), ("f16", "f16")])
