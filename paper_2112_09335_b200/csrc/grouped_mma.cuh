@@ -79,11 +79,11 @@ __device__ __forceinline__ uint32_t instruction(bool bf16) {
 __device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-      "mov.b64 da, {%1, %6};\n\t"
-      "mov.b64 db, {%2, %6};\n\t"
+      "mov.b64 da, {%1, %5};\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(0u), "r"(kDescHi)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
       : "memory");
 }
 // The same for a pair of blocks, M = 256: by one thread of the first block, for both.
