@@ -399,9 +399,17 @@ struct gcn_admm {
       CU(cudaStreamIsCapturing(stream, &capture));
       if (capture != cudaStreamCaptureStatusNone)
         throw Fail{GCN_ADMM_ERR_ARG, "the workspace would have to grow, which a stream that is being captured does not allow: make the call once before"};
-      const size_t count = std::max(tickets, work_tickets);
+      const size_t count = std::max<size_t>({tickets, work_tickets, 512}), had = work.size - std::min(work.size, behind(work_tickets));
       old_work.reserve(old_work.size() + 1);
-      gcn_admm_mem::Slab larger = take_slab(behind(count) + std::max(bytes, work.size - std::min(work.size, behind(work_tickets))));
+      // by half at least where there is memory for it: what has been outgrown is then no more than twice what is there
+      gcn_admm_mem::Slab larger;
+      try {
+        larger = take_slab(behind(count) + std::max(bytes, had + had / 2));
+      } catch (const Fail& f) {
+        if (f.code != GCN_ADMM_ERR_ALLOC || bytes >= had + had / 2) throw;
+        cudaGetLastError();
+        larger = take_slab(behind(count) + std::max(bytes, had));
+      }
       if (work.base) old_work.push_back({work, work_tickets});
       work = larger;
       work_tickets = count;

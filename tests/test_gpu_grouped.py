@@ -606,6 +606,26 @@ def test_a_first_call_may_be_captured():
         g.destroy()
 
 
+def test_a_growing_workspace_holds_a_bounded_amount():
+    """Calls that need a little more every time: the outgrown workspaces together are no more than twice the last one, and go with the handle."""
+    import torch
+    g = trainer()
+    try:
+        last = torch.randn(1, 2048, 2048, device="cuda")
+        out = torch.empty_like(last)
+        free = torch.cuda.mem_get_info()[0]
+        for side in range(256, 2049, 64):
+            g.orthogonalise(last.data_ptr(), out.data_ptr(), 1, side, side, [MUON], ldg=2048, ldo=2048)
+        torch.cuda.synchronize()
+        # images of X twice, S and P, two halves an element, and grain; half as much again as the step before may have taken
+        largest = 4 * 2 * 2 * 2048 * 2048
+        assert free - torch.cuda.mem_get_info()[0] <= 3 * 1.5 * largest + (64 << 20)
+        want = newton_schulz(last, [MUON], 1e-7, 1.0)
+        assert float((out.double() - want).norm() / want.norm()) < ortho_tolerance(last, [MUON], out.dtype)
+    finally:
+        g.destroy()
+
+
 def test_two_handles_at_once():
     """Handles on streams of their own share nothing: the same calls side by side give what they give alone."""
     import torch
