@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 SOURCES = [os.path.join(HERE, "csrc", "gcn_admm.cu"), os.path.join(HERE, "csrc", "grouped.cu")]
 HEADERS = [os.path.join(HERE, "csrc", "kernels.cuh"), os.path.join(HERE, "csrc", "gemm_half.cuh"), os.path.join(HERE, "csrc", "gemm_tc.cuh"), os.path.join(HERE, "csrc", "graph_index.hpp"), os.path.join(HERE, "csrc", "shard_plan.hpp"), os.path.join(HERE, "csrc", "memory.hpp"),
-           os.path.join(HERE, "csrc", "grouped.hpp"), os.path.join(HERE, "csrc", "grouped_plan.hpp"), os.path.join(HERE, "csrc", "grouped_mma.cuh"), os.path.join(HERE, "csrc", "tensor_map.hpp"),
+           os.path.join(HERE, "csrc", "grouped.hpp"), os.path.join(HERE, "csrc", "grouped_plan.hpp"), os.path.join(HERE, "csrc", "grouped_mma.cuh"), os.path.join(HERE, "csrc", "grouped_words.hpp"), os.path.join(HERE, "csrc", "tensor_map.hpp"),
            os.path.join(os.path.dirname(HERE), "include", "gcn_admm.h")]
 LIB = os.path.join(HERE, "libgcn_admm.so")
 

@@ -31,6 +31,7 @@
 
 #include "gemm_tc.cuh"
 #include "grouped_plan.hpp"
+#include "grouped_words.hpp"
 
 namespace gcn_admm_grouped {
 
@@ -320,18 +321,18 @@ struct Raw<float> {
   }
 };
 // Halves on any boundary: the aligned words that hold them, as they are, until they are stored (124576 x 211 x 156: 146 us with a load for every half,
-// put together as it came, 120 us so).  A word that holds an element of a matrix lies in the matrix's allocation.
+// put together as it came, 120 us so).  A word that holds an element of a matrix lies in the matrix's allocation; other words are not touched.
 template <>
 struct Raw<unsigned short> {
   uint32_t v[5];
   int valid;   // elements, negative where the first is in the middle of a word
   template <bool>
   __device__ __forceinline__ void load(const unsigned short* p, int valid_) {
-    const uint32_t* const q = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
-    const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1), some = min(max(valid_, 0), 8);
-    valid = odd ? -some : some;
+    const HalfWords words(reinterpret_cast<uintptr_t>(p), valid_);
+    const uint32_t* const q = reinterpret_cast<const uint32_t*>(words.first);
+    valid = words.odd ? -words.some : words.some;
 #pragma unroll
-    for (int k = 0; k < 5; ++k) v[k] = 2 * k < some + odd ? __ldg(q + k) : 0u;
+    for (int k = 0; k < 5; ++k) v[k] = words.holds(k) ? __ldg(q + k) : 0u;
   }
   __device__ __forceinline__ void store(uint8_t* at, int) const {
     const int some = abs(valid);

@@ -1,0 +1,40 @@
+"""Words of memory that the grouped products load of operands off 16-byte boundaries (host code on its own; no GPU)."""
+import os
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def words(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("words") / "harness")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", os.path.join(HERE, "grouped_words_harness.cpp"), "-o", exe], check=True)
+
+    def run(cases):
+        out = subprocess.run([exe], input="".join(f"{a} {v}\n" for a, v in cases), capture_output=True, text=True, check=True).stdout.splitlines()
+        assert len(out) == len(cases)
+        return [[int(w) for w in line.split()] for line in out]
+    return run
+
+
+def test_every_word_holds_a_valid_half_and_every_valid_half_has_its_word(words):
+    cases = [(4096 + 2 * shift, valid) for shift in range(16) for valid in range(-200, 12)]
+    for (address, valid), got in zip(cases, words(cases)):
+        halves = [address + 2 * e for e in range(max(0, min(valid, 8)))]
+        assert got == sorted({h & ~3 for h in halves}), (address, valid)
+
+
+@pytest.mark.parametrize("rows, width, ld, base", [(1, 767, 767, 0), (129, 767, 767, 2), (65, 5, 5, 0), (3, 9, 1001, 6)])
+def test_a_tile_of_rows_stays_inside_of_its_matrix(words, rows, width, ld, base):
+    """Every unit of 128-row tiles over a matrix whose allocation ends with its last element: rows behind the last and columns behind the width included."""
+    start, end = 1 << 20, (1 << 20) + base + 2 * ((rows - 1) * ld + width)
+    cases = []
+    for row in range((rows + 127) // 128 * 128):
+        for col in range(0, (width + 63) // 64 * 64, 8):
+            cases.append((start + base + 2 * (row * ld + col), width - col if row < rows else 0))
+    for (address, valid), got in zip(cases, words(cases)):
+        for w in got:
+            # a word is inside where one of its halves is: allocations begin and end on words
+            assert start + base - 2 <= w < end, (address, valid)
