@@ -304,7 +304,7 @@ struct Raw<float> {
     }
   }
   // The three parts, `part` bytes apart: each the upper half of what the last ones leave (differences are exact).
-  __device__ __forceinline__ void store(uint8_t* at, int part) const {
+  __device__ __forceinline__ void store(uint8_t* at, long long part) const {
     uint32_t w[3][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -317,7 +317,7 @@ struct Raw<float> {
       }
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(at + k * part) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(at + part_at(k, part)) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
   }
 };
 // Halves on any boundary: the aligned words that hold them, as they are, until they are stored (124576 x 211 x 156: 146 us with a load for every half,
@@ -334,7 +334,7 @@ struct Raw<unsigned short> {
 #pragma unroll
     for (int k = 0; k < 5; ++k) v[k] = words.holds(k) ? __ldg(q + k) : 0u;
   }
-  __device__ __forceinline__ void store(uint8_t* at, int) const {
+  __device__ __forceinline__ void store(uint8_t* at, long long) const {
     const int some = abs(valid);
     uint32_t w[4];
 #pragma unroll

@@ -19,4 +19,7 @@ struct HalfWords {
   GROUPED_BOTH bool holds(int word) const { return some > 0 && 2 * word < some + odd; }
 };
 
+// Byte offset of part k of an element whose parts lie `apart` bytes from each other (images of split weights are longer than an int counts).
+GROUPED_BOTH long long part_at(int k, long long apart) { return k * apart; }
+
 }  // namespace gcn_admm_grouped

@@ -1,0 +1,30 @@
+"""Products grouped by expert and orthogonalised updates where sizes and values reach the limits of their formats.  Tolerances of products: those of
+test_gpu_grouped.py."""
+import pytest
+
+from paper_2112_09335_b200 import binding
+from test_gpu_grouped import bound, h, offsets_of  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def test_weights_whose_split_images_pass_31_bits(h):  # noqa: F811
+    """Two fp32 weights of 32768 x 16400: a part of their images is 2^31 bytes and more, so that parts 1 and 2 lie farther than an int reaches."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k, n, sizes = 32768, 16400, [300, 290]
+    rows = sum(sizes)
+    x = torch.randn(rows, k, generator=gen, device="cuda")
+    w = torch.empty(2, k, n, device="cuda").normal_(generator=gen)
+    y = torch.full((rows, n), 7.0, device="cuda")
+    off = offsets_of(sizes)
+    h.grouped_product(x.data_ptr(), w.data_ptr(), y.data_ptr(), off.data_ptr(), 2, rows, k, n)
+    torch.cuda.synchronize()
+    at = 0
+    for g, size in enumerate(sizes):
+        a = x[at:at + size].double()
+        for lo in (0, n // 2 - 3, n - 130):
+            b = w[g, :, lo:lo + 130].double()
+            got, want = y[at:at + size, lo:lo + 130], a @ b
+            assert not bool(((got.double() - want).abs() > bound(got, want, a.abs() @ b.abs(), k)).any())
+        at += size

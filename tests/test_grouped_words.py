@@ -12,8 +12,8 @@ def words(tmp_path_factory):
     exe = str(tmp_path_factory.mktemp("words") / "harness")
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", os.path.join(HERE, "grouped_words_harness.cpp"), "-o", exe], check=True)
 
-    def run(cases):
-        out = subprocess.run([exe], input="".join(f"{a} {v}\n" for a, v in cases), capture_output=True, text=True, check=True).stdout.splitlines()
+    def run(cases, what="w"):
+        out = subprocess.run([exe], input="".join(f"{what} {a} {v}\n" for a, v in cases), capture_output=True, text=True, check=True).stdout.splitlines()
         assert len(out) == len(cases)
         return [[int(w) for w in line.split()] for line in out]
     return run
@@ -38,3 +38,9 @@ def test_a_tile_of_rows_stays_inside_of_its_matrix(words, rows, width, ld, base)
         for w in got:
             # a word is inside where one of its halves is: allocations begin and end on words
             assert start + base - 2 <= w < end, (address, valid)
+
+
+def test_parts_of_images_longer_than_31_bits(words):
+    """Images of 1024 weights of 1024 x 1024 fp32 elements and more: part 1 lies 2^31 bytes behind part 0, part 2 twice as far."""
+    cases = [(k, apart) for apart in (16384, (1 << 30) + 16, (1 << 31) - 16, 1 << 31, 3 << 31, 1 << 38) for k in range(3)]
+    assert words(cases, "p") == [[k * apart] for k, apart in cases]
