@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   const uint32_t tmem = tmem_slot;
   volatile int* const abortp = &abort_flag;
   const int segment = job.segment();
-  int copies = 0;   // stages this thread has started copies into
+  CopyLog copies;   // of this thread
   typename J::Item it;
   typename J::Walk walk = job.start(worker, workers);
 
@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
             // a chunk with rows to clear is announced to the warp that does it
             else if (J::kTailed && it.tail < kBK && c + 1 == it.chunks) job.template copy<false>(it, c, tile, tail + 8 * slot);
             else job.template copy<PAIR>(it, c, tile, full_there + 8 * slot);
-            ++copies;
+            copies.add(slot, J::kTailed && it.tail < kBK && c + 1 == it.chunks);
             if (++slot == S) { slot = 0; parity ^= 1u; }
           }
         }
@@ -647,9 +647,23 @@ __global__ void __launch_bounds__(GeometryOf<J>::kThreads, 1) k_products(const _
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if (abort_flag) {   // what is still in flight is waited for before shared and tensor memory are let go
+  if (abort_flag) {
+    // What is still in flight is waited for before shared and tensor memory are let go: each copy at the barrier that it reports to, with a bound (a phase
+    // that also waits for what never came does not end).  Copies of a pair's second block report to the first one's barriers, on which
+    // only that one can wait: there the bound itself, a thousand times what a copy takes, has to do.  A block of a pair that has not given up has
+    // seen the end of every copy and instruction, its own and those that the other block issued for it.
     if (tid == 0) atomicOr(job.error_flag(), 1);
-    if (warp == kMmaWarp + 1 && lane == 0 && (J::kTma || J::kTmaB) && rank == 0) gtc::drain_copies(full, S, copies);
+    if (warp == kMmaWarp + 1 && lane == 0 && (J::kTma || J::kTmaB)) {
+      bool unseen = false;
+      for (int i = max(0, copies.started - S); i < copies.started; ++i) {
+        const int slot = i % S;
+        if (J::kTailed && copies.is_tail(slot)) gtc::drain_wait(tail + 8 * slot, copies.tail_parity(slot));
+        else if (rank == 0) gtc::drain_wait(full + 8 * slot, CopyLog::full_parity(i, S));
+        else unseen = true;
+      }
+      if (PAIR && unseen)
+        for (const long long t0 = clock64(); clock64() - t0 < gtc::kDrainClocks;) {}
+    }
     if (warp == kMmaWarp && lane == 0 && rank == 0) {
       if constexpr (PAIR) {
         commit_pair(drain);

@@ -1,5 +1,6 @@
 """Words of memory that the grouped products load of operands off 16-byte boundaries (host code on its own; no GPU)."""
 import os
+import random
 import subprocess
 
 import pytest
@@ -44,3 +45,17 @@ def test_parts_of_images_longer_than_31_bits(words):
     """Images of 1024 weights of 1024 x 1024 fp32 elements and more: part 1 lies 2^31 bytes behind part 0, part 2 twice as far."""
     cases = [(k, apart) for apart in (16384, (1 << 30) + 16, (1 << 31) - 16, 1 << 31, 3 << 31, 1 << 38) for k in range(3)]
     assert words(cases, "p") == [[k * apart] for k, apart in cases]
+
+
+def test_each_copy_in_flight_is_known_by_its_barrier_and_phase(words):
+    """Sequences of copies, those with rows behind an item at random places: the k-th use of a barrier ends its phase k, of parity k mod 2."""
+    rng = random.Random(3)
+    cases = [(slots, 1 << n | rng.getrandbits(n) if n else 1) for slots in (1, 2, 4, 6, 8) for n in (0, 1, 2, 5, 7, 12, 30, 55) for _ in range(20)]
+    for (slots, flags), got in zip(cases, words(cases, "c")):
+        tails = [flags >> i & 1 for i in range(flags.bit_length() - 1)]
+        want = []
+        for i in range(max(0, len(tails) - slots), len(tails)):
+            before = range(i % slots, i, slots)            # earlier copies of this slot
+            uses = sum(tails[j] for j in before) if tails[i] else len(before)
+            want += [i % slots, tails[i], uses % 2]
+        assert got == want, (slots, flags)
