@@ -195,7 +195,7 @@ int gcn_admm_dense_product_tn(gcn_admm* h, const float* A, const float* B, float
  * handle's communities, in the order of gcn_admm_index (n_groups and rows must then be the handle's).  Groups should not overlap (rows of two
  * groups get one of the two results).  Results may not alias operands.
  * All work is enqueued on the handle's stream; the calls return without synchronising, may be captured, and give the same bits
- * every time.  gcn_admm_grouped_product (fp32, many rows: its weights as three parts), gcn_admm_grouped_product_tn and
+ * every time.  gcn_admm_grouped_product (fp32, many rows: its weights as three parts; where there is no memory for them every tile splits its own, slower and with the same bits), gcn_admm_grouped_product_tn and
  * gcn_admm_orthogonalise use a workspace of the handle that grows when a call needs more of it: the first call of a size allocates and may not be
  * part of a capture (it is refused there); what it was before stays with the handle, for graphs that hold it.  Calls, and replays of captured ones, that share a handle must follow one another on its stream.  A bounded wait that runs out on the device is reported like that of any product (see
  * GCN_ADMM_ST_PIPELINE_FLAG). */

@@ -1967,7 +1967,16 @@ int gcn_admm_grouped_product(gcn_admm* h, int type, const void* x, long long ldx
     p.offsets = offsets_or_communities(h, offsets, n_groups, rows);
     if (rows == 0) return;
     h->need_device({x, w, y, offsets});
-    const gcn_admm_grouped::Room room = h->room_for(gcn_admm_grouped::space_bytes(p), 0);
+    const gcn_admm_grouped::Room room = [&] {
+      try {
+        return h->room_for(gcn_admm_grouped::space_bytes(p), 0);
+      } catch (const Fail& f) {
+        if (f.code != GCN_ADMM_ERR_ALLOC) throw;
+        cudaGetLastError();
+        p.unsplit = true;   // the images are for speed only: the same results, bit for bit, come without them
+        return h->room_for(gcn_admm_grouped::space_bytes(p), 0);
+      }
+    }();
     char name[48];
     std::snprintf(name, sizeof name, "grouped@%dx%d", k, n);
     const int size = gcn_admm_grouped::size_of(type);

@@ -1060,7 +1060,7 @@ std::size_t space_bytes(const Orthogonal& p) { return is_small(p) ? 0 : Orthogon
 // Whether the weights are split beforehand: where there are at least two tiles of rows to a group they would be split again for every one.
 bool splits_weights(const Product& p) {
   const long long w_rows = p.transposed ? p.n : p.k, w_cols = p.transposed ? p.k : p.n;
-  return p.type == kF32 && p.rows >= 2LL * kBM * p.groups && w_rows * cdiv(w_cols, 8) < INT_MAX && gcn_admm_host::encode_tiled() != nullptr;
+  return p.type == kF32 && !p.unsplit && p.rows >= 2LL * kBM * p.groups && w_rows * cdiv(w_cols, 8) < INT_MAX && gcn_admm_host::encode_tiled() != nullptr;
 }
 std::size_t space_bytes(const Product& p) {
   if (!splits_weights(p)) return 0;

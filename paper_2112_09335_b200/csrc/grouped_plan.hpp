@@ -34,6 +34,7 @@ struct Product {
   int k, n;
   void* y;
   long long ldy;
+  bool unsplit = false;   // no room for images of fp32 weights: every tile splits them for itself
 };
 // dw_g = sum of x[i]^T y[i] over the rows of group g.
 struct ProductTn {

@@ -3,7 +3,7 @@ test_gpu_grouped.py."""
 import pytest
 
 from paper_2112_09335_b200 import binding
-from test_gpu_grouped import bound, h, offsets_of  # noqa: F401
+from test_gpu_grouped import bound, h, offsets_of, trainer  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,34 @@ def test_weights_whose_split_images_pass_31_bits(h):  # noqa: F811
             got, want = y[at:at + size, lo:lo + 130], a @ b
             assert not bool(((got.double() - want).abs() > bound(got, want, a.abs() @ b.abs(), k)).any())
         at += size
+
+
+def test_fp32_products_without_room_for_split_weights():
+    """Images of fp32 weights are for speed: where there is no memory for them the call gives the same bits without."""
+    import torch
+    k, n, groups, rows = 4096, 8192, 8, 2100
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(rows, k, generator=gen, device="cuda")
+    w = torch.empty(groups, k, n, device="cuda").normal_(generator=gen)
+    y = [torch.zeros(rows, n, device="cuda") for _ in range(2)]
+    off = offsets_of([300] * 6 + [0, 300])
+    images, hog = 3 * groups * k * n * 2, None
+    try:
+        for i in range(2):
+            g = trainer()
+            try:
+                if i == 1:      # memory for half of them is left
+                    torch.cuda.empty_cache()
+                    hog = torch.empty(torch.cuda.mem_get_info()[0] - images // 2, dtype=torch.uint8, device="cuda")
+                    assert torch.cuda.mem_get_info()[0] < images
+                g.grouped_product(x.data_ptr(), w.data_ptr(), y[i].data_ptr(), off.data_ptr(), groups, rows, k, n)
+                torch.cuda.synchronize()
+            finally:
+                g.destroy()
+                binding.release_idle()
+    finally:
+        del hog
+        torch.cuda.empty_cache()
+    a, b = x[:300].double(), w[0, :, :200].double()
+    assert not bool(((y[0][:300, :200].double() - a @ b).abs() > bound(y[0][:300, :200], a @ b, a.abs() @ b.abs(), k)).any())
+    assert torch.equal(y[0], y[1])
