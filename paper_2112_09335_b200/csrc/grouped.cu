@@ -471,7 +471,8 @@ struct ProductTnJob {
 //    rounding is 1.7e-3 of the result: five steps end 0.5 to 0.8e-3 off (1.3e-3 where 280 of 300 singular values are 1e-3 of the rest), in a third of the
 //    instructions.  With the diagonals inside it is 1.3 to 1.8e-3, with X in halves only 1e-3 to 4e-2: the steps lift small singular values, and what they are off, by |a| each.
 // Matrices between products are images: part hi of all matrices, then part lo, rows padded to 32 bytes, under a power of two that comes from
-// the bounds of the singular values (host, grow()): entries stay below 2^15 and far above the smallest half.  S and P are symmetric: only
+// the bounds of the singular values (step_factors(), for each matrix from its own norm: beside eps it may be tiny): entries stay below 2^15 and
+// far above the smallest half.  S and P are symmetric: only
 // tiles that reach the diagonal are formed, the others are written turned.  X keeps its own orientation throughout, so nothing is transposed.
 struct Image {
   __half* at;
@@ -510,11 +511,33 @@ __global__ void __launch_bounds__(256) k_norm(const Orthogonal p, bool vec, doub
   }
 }
 
-// X_0 = G / (||G|| + eps), to its image under `scale`; with no steps to take, `scale` times it, to the result.  A thread has eight elements of a row.
+struct Steps {
+  int count;
+  float c[3 * kMaxSteps];
+};
+// What the three products of each step multiply the sums and matrices of a matrix with: StepFactors, one float4 each.
+struct Factors {
+  float4* at;
+  int batch;
+  __host__ __device__ __forceinline__ float4* of(int step, int stage) const { return at + ((size_t)step * 3 + stage) * batch; }
+};
+
+// X_0 = G / (||G|| + eps), to its image; with no steps to take, p.scale times it, to the result.  A thread has eight elements of a row at a time.  The last
+// block of each matrix follows the scales through the steps meanwhile.
+constexpr int kStartBlocks = 8 * kSms;   // of all matrices together, or one for each: finding out a scale costs a block more than 2048 elements (16 of
+// 1024 x 2048: 60 us with a block for every 2048 elements, 38 so)
 template <typename T, typename O>
-__global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, const double* __restrict__ partial, int partials, const Image x, float scale) {
+__global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, const double* __restrict__ partial, int partials, const Image x, const __grid_constant__ Steps steps,
+                                               const Factors factors) {
   gtc::enter_kernel();
   __shared__ double s_sum[8];
+  __shared__ Stationary s_at[kMaxSteps];
+  __shared__ double s_most[kMaxSteps];
+  const unsigned blocks = gridDim.x - 1;
+  if (blockIdx.x == blocks && (int)threadIdx.x < steps.count) {
+    const float* const c = steps.c + 3 * threadIdx.x;
+    s_at[threadIdx.x] = stationary(c[0], c[1], c[2]);
+  }
   double sum = (int)threadIdx.x < partials ? partial[blockIdx.y * kNormBlocks + threadIdx.x] : 0.0;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -525,14 +548,34 @@ __global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, con
   const double norm = sqrt(sum) + (double)p.eps;
   // a zero matrix stays zero, one that is not finite becomes NaN
   const double inverse = !(norm > 0.0) ? (sum == 0.0 ? 0.0 : nan("")) : norm < INFINITY ? 1.0 / norm : nan("");
+  const double first = first_bound(sqrt(sum) * inverse);
+  if (blockIdx.x == blocks) {
+    double most = first;
+    for (int i = 0; threadIdx.x == 0 && i < steps.count; ++i) {
+      s_most[i] = most;
+      most = bound_behind(grow(most, steps.c[3 * i], steps.c[3 * i + 1], steps.c[3 * i + 2], s_at[i]));
+    }
+    __syncthreads();
+    const int i = (int)threadIdx.x;
+    if (i < steps.count) {
+      const float* const c = steps.c + 3 * i;
+      const StepFactors f = step_factors(s_most[i], grow(s_most[i], c[0], c[1], c[2], s_at[i]), c[0], c[1], c[2], i + 1 == steps.count, p.scale, std::is_same_v<O, __nv_bfloat16>);
+      factors.of(i, 0)[blockIdx.y] = make_float4(f.gram, 0.f, 0.f, 0.f);
+      factors.of(i, 1)[blockIdx.y] = make_float4(f.square, f.linear, f.diagonal, f.unscale);
+      factors.of(i, 2)[blockIdx.y] = make_float4(f.move, f.own, 0.f, 0.f);
+    }
+    return;
+  }
+  const double by = x.at != nullptr ? ldexp(inverse, scale_for(first)) : inverse;
+  const float scale = x.at != nullptr ? 1.f : p.scale;
   const T* const g = static_cast<const T*>(p.g) + (long long)blockIdx.y * p.stride_g;
   const unsigned units = x.ld / 8, count = (unsigned)p.rows * units;
-  for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += gridDim.x * 256) {
+  for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < count; e += blocks * 256) {
     const unsigned row = e / units, col = (e - row * units) * 8;
     float v[8];
     load8(g + row * p.ldg + col, p.cols - (int)col, vec, v);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (float)((double)v[k] * inverse) * scale;
+    for (int k = 0; k < 8; ++k) v[k] = (float)((double)v[k] * by) * scale;
     if (x.at != nullptr) {
       uint32_t hi[4], lo[4];
 #pragma unroll
@@ -559,17 +602,13 @@ __global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, con
 // every step is three launches of tiles that are nearly empty: eight matrices of 128 x 16 took 73 us, 16 us so.)
 // X lies as [n][M], its shorter side, padded to M, contiguous.  S: every warp adds up the products of its part of the n steps, a lane the M / 8 x M / 4
 // entries at its place, and the warps' sums are added in order.  X <- P X: a thread has columns of its own and reads P, the same for all.
-struct SmallSteps {
-  int count;
-  float c[3 * kMaxSteps];
-};
 constexpr int kSmallSide = 32, kSmallThreads = 512, kSmallBytes = 160 * 1024;
 template <int M>
 constexpr size_t small_bytes(int n) {
   return ((size_t)n * M + (kSmallThreads / 32) * M * M + 2 * M * M) * sizeof(float);
 }
 template <int M, typename T, typename O>
-__global__ void __launch_bounds__(kSmallThreads) k_small(const Orthogonal p, const __grid_constant__ SmallSteps steps) {
+__global__ void __launch_bounds__(kSmallThreads) k_small(const Orthogonal p, const __grid_constant__ Steps steps) {
   gtc::enter_kernel();
   constexpr int kWarps = kSmallThreads / 32, TI = M / 8, TJ = M / 4;
   extern __shared__ __align__(16) float small_smem[];
@@ -679,12 +718,10 @@ struct OrthogonalArgs {
   CUtensorMap a, b;
   int* error_flag;
   int batch, rows, cols, k;     // of the products: D is rows x cols, the reduction has k steps
-  float factor;                 // of the sums, for what is stored
-  float diagonal, linear;       // kPolynomial: a, under the scale of P where it is in P; b under that of P over that of S.  kMove: the scale of the result over that of X
+  const float4* factors;        // of every matrix, for this stage
   Image s, to;                  // kPolynomial: S, kMove: X; where the result goes
   const float* diagonals;       // 1 part, kPolynomial: of S (under its scale), kMove: a + those of P
   float* to_diagonals;          // 1 part: where those of the result go
-  float unscale;                // 1 part, kPolynomial: one over the scale of P
   void* out;                    // last kMove: the caller's matrix
   int out_type;
   long long ldo, stride_o;
@@ -774,7 +811,9 @@ struct OrthogonalJob {
   struct Block {
     uint32_t hi[16], lo[reads_low() ? 16 : 1];
   };
-  using Early = std::conditional_t<kReads, Block, Nothing>;
+  struct Early : std::conditional_t<kReads, Block, Nothing> {
+    float4 factors;   // of the matrix, on their way while its products are formed
+  };
   __device__ __forceinline__ void fetch(const Item& it, int row, int col, Block& b) const {
     const __half* const at = a.s.matrix(it.matrix) + (long long)row * a.s.ld + col;
 #pragma unroll
@@ -792,6 +831,7 @@ struct OrthogonalJob {
     }
   }
   __device__ __forceinline__ void early(const Item& it, int warp, Early& b) const {
+    b.factors = __ldg(a.factors + it.matrix);
     if constexpr (kReads) fetch(it, it.row0 + (warp & 3) * 32 + (threadIdx.x & 31), it.col0 + (warp >> 2) * (BN / 2), b);
   }
   __device__ __forceinline__ static float2 floats(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
@@ -809,6 +849,9 @@ struct OrthogonalJob {
     const int row0 = it.row0 + (warp & 3) * 32, col0 = it.col0 + (warp >> 2) * NC, lane = threadIdx.x & 31, row = row0 + lane;
     const int rows_left = a.rows - row0, cols_left = a.cols - col0;
     if (rows_left <= 0 || cols_left <= 0) return;
+    const float4 factors = next.factors;
+    // of the sums; of S or X; of the diagonal of P, and what takes its scale off
+    const float factor = factors.x, linear = factors.y, on_diagonal = factors.z, unscale = factors.w;
     const bool diagonal = kSymmetric && row0 < col0 + NC && col0 < row0 + 32;   // whether the warp holds some of it
     // 1 part: the diagonal entry of this lane's row, and those of the columns, NC / 32 a lane
     constexpr bool kTall = STAGE == kMove && !B_MN;
@@ -831,14 +874,14 @@ struct OrthogonalJob {
       if (c0 < cols_left) {
         float x[32];
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = acc[c0 + c] * a.factor;
+        for (int c = 0; c < 32; ++c) x[c] = acc[c0 + c] * factor;
         if constexpr (kReads) {
-          const Block now = next;
+          const Block now = static_cast<const Block&>(next);
           if (c0 + 32 < NC) fetch(it, row, col0 + c0 + 32, next);
           // of S b, with its diagonals apart b + c (D_i + D_j); of X the diagonal of P and a
           const auto weight = [&](int c) {
-            if (STAGE == kPolynomial) return PARTS == 1 ? fmaf(a.factor, mine + __shfl_sync(0xffffffffu, theirs[c0 / 32], c), a.linear) : a.linear;
-            return (kTall ? __shfl_sync(0xffffffffu, theirs[c0 / 32], c) : mine) * a.linear;
+            if (STAGE == kPolynomial) return PARTS == 1 ? fmaf(factor, mine + __shfl_sync(0xffffffffu, theirs[c0 / 32], c), linear) : linear;
+            return (kTall ? __shfl_sync(0xffffffffu, theirs[c0 / 32], c) : mine) * linear;
           };
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
@@ -856,9 +899,9 @@ struct OrthogonalJob {
           for (int c = 0; c < 32; ++c) {
             if (row == col0 + c0 + c) {
               if constexpr (PARTS == 2) {
-                if (STAGE == kPolynomial) x[c] += a.diagonal;
+                if (STAGE == kPolynomial) x[c] += on_diagonal;
               } else {   // the image has none: O O alone is in x, b D + c D D is added
-                if (STAGE == kPolynomial) x[c] = fmaf(fmaf(fmaf(a.factor, mine, a.linear), mine, x[c]), a.unscale, a.diagonal);
+                if (STAGE == kPolynomial) x[c] = fmaf(fmaf(fmaf(factor, mine, linear), mine, x[c]), unscale, on_diagonal);
                 if (row < a.rows) a.to_diagonals[(long long)it.matrix * a.rows + row] = x[c];
                 x[c] = 0.f;
               }
@@ -1030,6 +1073,7 @@ struct OrthogonalSpace {
   double* partial;
   Image x[2], s, p;
   float *s_diagonals, *p_diagonals;
+  Factors factors;
   std::size_t bytes;
   OrthogonalSpace(const Orthogonal& o, void* space) {
     const int m = std::min(o.rows, o.cols);
@@ -1051,6 +1095,7 @@ struct OrthogonalSpace {
     p = image(m, m);
     s_diagonals = static_cast<float*>(take((std::size_t)o.batch * m * sizeof(float)));
     p_diagonals = static_cast<float*>(take((std::size_t)o.batch * m * sizeof(float)));
+    factors = Factors{static_cast<float4*>(take((std::size_t)o.steps * 3 * o.batch * sizeof(float4))), o.batch};
     bytes = used;
   }
 };
@@ -1159,6 +1204,13 @@ cudaError_t enqueue(const ProductTn& p, const Room& room) {
   });
 }
 
+Steps steps_of(const Orthogonal& p) {
+  Steps s{};
+  s.count = p.steps;
+  if (p.steps > 0) std::copy(p.coefficients, p.coefficients + 3 * p.steps, s.c);
+  return s;
+}
+
 // One block a matrix, where it fits (see k_small).
 bool is_small(const Orthogonal& p) {
   const int m = std::min(p.rows, p.cols), n = std::max(p.rows, p.cols);
@@ -1166,9 +1218,7 @@ bool is_small(const Orthogonal& p) {
 }
 template <int M>
 cudaError_t enqueue_small(const Orthogonal& p, const Room& room) {
-  SmallSteps steps{};
-  steps.count = p.steps;
-  if (p.steps > 0) std::copy(p.coefficients, p.coefficients + 3 * p.steps, steps.c);
+  const Steps steps = steps_of(p);
   const size_t smem = small_bytes<M>(std::max(p.rows, p.cols));
   cudaError_t e = cudaSuccess;
   with_types(p.type, p.out_type, [&](auto in, auto out) {
@@ -1185,18 +1235,16 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
   const bool tall = p.rows > p.cols;
   const OrthogonalSpace at(p, room.space);
   const Image none{nullptr, p.rows, at.x[0].ld, 0};
-  // the power of two that keeps numbers up to `most` below 2^15
-  const auto scale_for = [](double most) { return std::ldexp(1.0, 14 - std::ilogb(most)); };
-  double most = 1.0, scale = p.steps > 0 ? scale_for(most) : (double)p.scale;
   const long long elements = (long long)p.rows * p.cols;
   const int partials = (int)std::min<long long>(kNormBlocks, cdiv(elements, 4096));
   const bool vec = even(p.g, p.ldg, size_of(p.type)) && (p.batch == 1 || p.stride_g * size_of(p.type) % 16 == 0);
   cudaError_t e = cudaSuccess;
   with_type(p.type, [&](auto in) { e = launch_plain(k_norm<decltype(in)>, dim3((unsigned)partials, (unsigned)p.batch), room, p, vec, at.partial); });
   if (e != cudaSuccess) return e;
+  const unsigned start_blocks = (unsigned)std::min<long long>(cdiv(kStartBlocks, p.batch), cdiv(elements, 2048));
   with_types(p.type, p.out_type, [&](auto in, auto out) {
-    e = launch_plain(k_start<decltype(in), decltype(out)>, dim3((unsigned)std::min<long long>(1024, cdiv(elements, 2048)), (unsigned)p.batch), room, p, vec, at.partial, partials,
-                     p.steps > 0 ? at.x[0] : none, (float)scale);
+    e = launch_plain(k_start<decltype(in), decltype(out)>, dim3(start_blocks + 1, (unsigned)p.batch), room, p, vec, at.partial, partials,
+                     p.steps > 0 ? at.x[0] : none, steps_of(p), at.factors);
   });
   const bool halves = p.out_type == kBf16;   // one part is enough
   const auto map = [&](CUtensorMap* t, const Image& im, int cols, int box_rows) {
@@ -1206,12 +1254,7 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
   const auto triangle = [&](int rows) { return p.batch * (cdiv(m, rows) * (cdiv(m, rows) + 1) / 2); };
   const int bn = halves && triangle(256) >= kSms / 2 ? 256 : triangle(128) >= kSms ? 128 : 64;
   for (int i = 0; i < p.steps && e == cudaSuccess; ++i) {
-    const float* const c = p.coefficients + 3 * i;
-    const Growth g = grow(most, c[0], c[1], c[2]);
-    const double scale_s = scale_for(most * most), scale_p = scale_for(std::max(g.factor, 1e-3));
-    const double next = std::max(g.value, 1e-3), scale_next = scale_for(next);
     const bool last = i + 1 == p.steps;
-    const double scale_to = last ? (double)p.scale : scale_next;
     const Image &x = at.x[i & 1], &y = at.x[(i + 1) & 1];
     const auto product = [&](auto tag, OrthogonalArgs& a) {
       using J = typename decltype(tag)::Type;
@@ -1224,14 +1267,11 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
     OrthogonalArgs gram{}, poly{}, move{};
     gram.rows = gram.cols = m;
     gram.k = tall ? p.rows : p.cols;
-    gram.factor = (float)(scale_s / (scale * scale));
+    gram.factors = at.factors.of(i, 0);
     gram.to = at.s;
     gram.to_diagonals = at.s_diagonals;
     poly.rows = poly.cols = poly.k = m;
-    poly.factor = (float)(c[2] * scale_p / (scale_s * scale_s));
-    poly.diagonal = (float)(halves ? c[0] : c[0] * scale_p);
-    poly.unscale = (float)(1.0 / scale_p);
-    poly.linear = (float)(c[1] * scale_p / scale_s);
+    poly.factors = at.factors.of(i, 1);
     poly.s = at.s;
     poly.to = at.p;
     poly.diagonals = at.s_diagonals;
@@ -1239,8 +1279,7 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
     move.rows = p.rows;
     move.cols = p.cols;
     move.k = m;
-    move.factor = (float)(scale_to / (scale_p * scale));
-    move.linear = (float)(scale_to / scale);
+    move.factors = at.factors.of(i, 2);
     move.s = x;
     move.to = y;
     move.diagonals = at.p_diagonals;
@@ -1271,8 +1310,6 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
       return step(parts, std::integral_constant<int, 128>());
     };
     e = halves ? wide(std::integral_constant<int, 1>()) : wide(std::integral_constant<int, 2>());
-    most = next;
-    scale = scale_next;
   }
   return e;
 }

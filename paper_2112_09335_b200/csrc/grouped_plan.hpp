@@ -1,10 +1,12 @@
 // Host side of the products grouped by expert and of the orthogonalised updates: what a call asks for, what is refused, and the
-// sizes of workspaces.  No CUDA in here, so that it can be tested on its own.
+// sizes of workspaces, and the scales of orthogonalised updates (computed on the device).  Nothing of CUDA in here, so that it can be tested on its own.
 #pragma once
 #include <algorithm>
 #include <cmath>
 #include <cstddef>
 #include <cstdint>
+
+#include "grouped_words.hpp"
 
 namespace gcn_admm_grouped {
 
@@ -106,22 +108,69 @@ inline const char* check(ProductTn& p) {
 struct Growth {
   double value, factor;
 };
-inline Growth grow(double most, double a, double b, double c) {
-  const auto factor = [&](double t) { return std::fabs(a + t * (b + t * c)); };
-  const auto value = [&](double s) { return s * factor(s * s); };
-  Growth g{value(most), std::max(factor(0.0), factor(most * most))};
-  const auto consider = [&](double t) {   // t = s^2 of a stationary point
-    if (t > 0.0 && t < most * most) g.value = std::max(g.value, value(std::sqrt(t)));
+// Where these may have their maxima beside the ends of the interval: up to two s of a step's value, one t = s^2 of its factor; below 0: none.
+struct Stationary {
+  double s[2], value[2], t, factor;
+};
+GROUPED_BOTH double step_factor(double t, double a, double b, double c) { return fabs(a + t * (b + t * c)); }
+GROUPED_BOTH Stationary stationary(double a, double b, double c) {
+  Stationary at{{-1.0, -1.0}, {0.0, 0.0}, -1.0, 0.0};
+  const auto consider = [&](int i, double t) {
+    if (!(t > 0.0)) return;
+    at.s[i] = sqrt(t);
+    at.value[i] = at.s[i] * step_factor(t, a, b, c);
   };
-  if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < most * most) g.factor = std::max(g.factor, factor(-b / (2.0 * c)));
-  const double d = 9.0 * b * b - 20.0 * a * c;   // of a + 3 b t + 5 c t^2
   if (c == 0.0) {
-    if (b != 0.0) consider(-a / (3.0 * b));
-  } else if (d >= 0.0) {
-    consider((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-    consider((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+    if (b != 0.0) consider(0, -a / (3.0 * b));
+    return at;
   }
+  if (-b / (2.0 * c) > 0.0) {
+    at.t = -b / (2.0 * c);
+    at.factor = step_factor(at.t, a, b, c);
+  }
+  const double d = 9.0 * b * b - 20.0 * a * c;   // of a + 3 b t + 5 c t^2
+  if (d >= 0.0) {
+    consider(0, (-3.0 * b + sqrt(d)) / (10.0 * c));
+    consider(1, (-3.0 * b - sqrt(d)) / (10.0 * c));
+  }
+  return at;
+}
+GROUPED_BOTH Growth grow(double most, double a, double b, double c, const Stationary& at) {
+  const double end = step_factor(most * most, a, b, c);
+  Growth g{most * end, fmax(fabs(a), end)};
+  for (int i = 0; i < 2; ++i)
+    if (at.s[i] > 0.0 && at.s[i] < most) g.value = fmax(g.value, at.value[i]);
+  if (at.t > 0.0 && at.t < most * most) g.factor = fmax(g.factor, at.factor);
   return g;
+}
+GROUPED_BOTH Growth grow(double most, double a, double b, double c) { return grow(most, a, b, c, stationary(a, b, c)); }
+
+// Scales of a matrix between its products: powers of two that bring what the bound of its singular values allows just below 2^15.  The bound starts from
+// ||G|| / (||G|| + eps), which only the device knows, rounded up to a power of two, and follows the steps; it is kept above 2^-96, and that of P above
+// 2^-400 (far below, fp32 results are zero for any `scale`), so that no factor leaves the range of fp32.
+constexpr int kLeastBound = -96;
+GROUPED_BOTH int scale_for(double most) { return 14 - ilogb(most); }   // the power of two
+GROUPED_BOTH double first_bound(double ratio) {
+  if (!(ratio > 0.0 && ratio < 1.0)) return 1.0;   // (a matrix of zeros or one that is not finite needs no scale)
+  int e;
+  if (frexp(ratio, &e) == 0.5) --e;
+  return ldexp(1.0, e < kLeastBound ? kLeastBound : e);
+}
+// What the products of a step do beside multiplying: S = gram (X X^T), P = square (S S) + linear S + diagonal I, X' = move (P X) + own X.
+struct StepFactors {
+  float gram;
+  float square, linear, diagonal, unscale;   // unscale: one over the scale of P
+  float move, own;                           // own: 1 part, beside the diagonals
+};
+GROUPED_BOTH double bound_behind(const Growth& g) { return fmax(g.value, 0x1p-96); }
+// Of a step from a bound of `most` that grows by g.  `last`: the result leaves under `out_scale` instead of its own.  `halves`: the diagonal of P is kept
+// apart, without its scale.
+GROUPED_BOTH StepFactors step_factors(double most, const Growth& g, double a, double b, double c, bool last, double out_scale, bool halves) {
+  const int x = scale_for(most), s = scale_for(most * most), p = scale_for(fmax(g.factor, 0x1p-400));
+  const double out = last ? out_scale : 1.0;
+  const int to = last ? 0 : scale_for(bound_behind(g));
+  return StepFactors{(float)ldexp(1.0, s - 2 * x), (float)ldexp(c, p - 2 * s), (float)ldexp(b, p - s), (float)(halves ? a : ldexp(a, p)),
+                     (float)ldexp(1.0, -p), (float)ldexp(out, to - p - x), (float)ldexp(out, to - x)};
 }
 constexpr double kMostValue = 16.0, kMostFactor = 1024.0;
 
@@ -147,7 +196,7 @@ inline const char* check(Orthogonal& p) {
     if (!std::isfinite(c[0]) || !std::isfinite(c[1]) || !std::isfinite(c[2])) return "a coefficient is not finite";
     const Growth g = grow(most, c[0], c[1], c[2]);
     if (g.value > kMostValue || g.factor > kMostFactor) return "the coefficients let singular values grow above 16, or their factors above 1024";
-    most = std::max(g.value, 1e-3);
+    most = std::max(g.value, std::ldexp(1.0, kLeastBound));
   }
   return nullptr;
 }

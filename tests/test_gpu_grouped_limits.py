@@ -3,7 +3,7 @@ test_gpu_grouped.py."""
 import pytest
 
 from paper_2112_09335_b200 import binding
-from test_gpu_grouped import bound, h, offsets_of, trainer  # noqa: F401
+from test_gpu_grouped import MUON, bound, code, h, newton_schulz, offsets_of, ortho_tolerance, torch_type, trainer  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,47 @@ def test_fp32_products_without_room_for_split_weights():
     a, b = x[:300].double(), w[0, :, :200].double()
     assert not bool(((y[0][:300, :200].double() - a @ b).abs() > bound(y[0][:300, :200], a @ b, a.abs() @ b.abs(), k)).any())
     assert torch.equal(y[0], y[1])
+
+
+def orthogonalised(h, g, coefficients, eps, scale, out):  # noqa: F811
+    import torch
+    names = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
+    x = torch.full(g.shape, float("nan"), dtype=torch_type(out), device="cuda")
+    h.orthogonalise(g.data_ptr(), x.data_ptr(), *g.shape, coefficients, eps=eps, scale=scale, type=code(names[g.dtype]), out_type=code(out))
+    return x
+
+
+SMALL = [(40, 24), (150, 200), (200, 70)]
+
+
+@pytest.mark.parametrize("kind, out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows, cols", SMALL + [(600, 520)])
+def test_norms_far_below_eps(h, kind, out, rows, cols):  # noqa: F811
+    """X_0 = G / (||G|| + eps) is then a tiny matrix, as accurate as any other: beside ordinary ones of the same batch, for coefficients with and without a."""
+    import torch
+    norms = [1.0, 1e-4, 1e-8, 1e-13, 1e-20, 1e-26]
+    g = torch.randn(len(norms), rows, cols, generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda", dtype=torch.float64)
+    g = (g / torch.linalg.norm(g, dim=(1, 2), keepdim=True) * torch.tensor(norms, device="cuda", dtype=torch.float64)[:, None, None]).to(torch_type(kind))
+    for coefficients in ([MUON] * 5, [(1.5, -0.5, 0.0)], [(0.0, 1.25, 0.0)], [(2.0, -1.5, 0.5)] * 12):
+        x = orthogonalised(h, g, coefficients, 1.0, 1.0, out)
+        want = newton_schulz(g, coefficients, 1.0, 1.0)
+        for i in range(len(norms)):
+            if float(want[i].norm()) < 1e-32:       # elements among the subnormal results
+                continue
+            rel = float((x[i].double() - want[i]).norm() / want[i].norm())
+            assert rel < ortho_tolerance(g[i:i + 1], coefficients, x.dtype, 1.0), (coefficients, norms[i], rel)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, cols", SMALL)
+def test_coefficients_that_make_everything_small(h, out, rows, cols):  # noqa: F811
+    import torch
+    g = torch.randn(2, rows, cols, generator=torch.Generator(device="cuda").manual_seed(cols), device="cuda").to(torch_type(out))
+    for coefficients, scale in (([(1e-7, 0.0, 0.0)] * 3, 1e21), ([(1e-9, 0.0, 0.0), MUON], 1e9), ([(0.0, 0.0, 1e-12)], 1e12), ([(0.0, 0.0, 0.0), MUON], 1.0)):
+        x = orthogonalised(h, g, coefficients, 1e-7, scale, out)
+        want = newton_schulz(g, coefficients, 1e-7, scale)
+        if float(want.norm()) == 0:
+            assert bool((x == 0).all())
+            continue
+        rel = float((x.double() - want).norm() / want.norm())
+        assert rel < ortho_tolerance(g, coefficients, x.dtype), (coefficients, rel)
