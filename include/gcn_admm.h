@@ -218,11 +218,9 @@ int gcn_admm_grouped_product_tn(gcn_admm* h, int type, const void* x, long long 
  * `batch` matrices G, rows x cols, X_0 = G / (||G||_F + eps) and n_steps times X <- a X + (b A + c A A) X with A = X X^T (X^T in place
  * of X where rows > cols); out = scale X.  coefficients: a, b, c of every step, host array of 3 n_steps floats.  Each singular value s
  * goes to s (a + b s^2 + c s^4); coefficients that let one grow above 16, or a factor a + b s^2 + c s^4 above 1024, are refused.  A
- * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  Results of fp32 and fp16 come from products to fp32 accuracy, by
+ * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  Results of every type come from products to fp32 accuracy, by
  * pairs of halves under scales of each matrix (its entries are bounded by its singular values, which start from at most ||G|| / (||G|| + eps): a matrix
- * whose norm is far below eps is as accurate as any, down to 2^-96 of it); results of bf16 from products of single halves with the
- * diagonals of A and of the polynomial, and a X, kept apart in fp32: 0.5 to 1.3e-3 of the result, beside 1.7e-3 of its rounding.  out may be g itself,
- * with the same type and strides. */
+ * whose norm is far below eps is as accurate as any, down to 2^-96 of it), and are rounded once.  out may be g itself, with the same type and strides. */
 int gcn_admm_orthogonalise(gcn_admm* h, int type, int batch, int rows, int cols, const void* g, long long ldg, long long stride_g,
                            int n_steps, const float* coefficients, float eps, float scale, int out_type, void* out, long long ldo,
                            long long stride_o);

@@ -464,12 +464,10 @@ struct ProductTnJob {
 };
 
 // ---- orthogonalised updates --------------------------------------------------------------------------
-// X <- P X with P = a I + b S + c S S, S = X X^T; for matrices taller than wide X <- X P with S = X^T X.  Three products a step, in two forms.
-//  2 parts: pairs of halves (three matrix instructions for one, 22 bits of each operand), for results of fp32 and fp16.
-//  1 part: operands are halves, but what is large is kept out of them: the diagonals of S and P stay in fp32 (S S of the rest O is
-//    O O + (D_i + D_j) O_ij), and X, a pair of halves, is itself multiplied by a + P_ii in fp32.  For results of bf16, whose
-//    rounding is 1.7e-3 of the result: five steps end 0.5 to 0.8e-3 off (1.3e-3 where 280 of 300 singular values are 1e-3 of the rest), in a third of the
-//    instructions.  With the diagonals inside it is 1.3 to 1.8e-3, with X in halves only 1e-3 to 4e-2: the steps lift small singular values, and what they are off, by |a| each.
+// X <- P X with P = a I + b S + c S S, S = X X^T; for matrices taller than wide X <- X P with S = X^T X.  Three products a step, of pairs of halves (three matrix
+// instructions for one, 22 bits of each operand), whatever the type of the result.  (Single halves are enough for the rounding of a bf16 result as long as it lasts a few
+// steps, but steps lift small singular values, and what they are off, by |a| each: ten steps of a matrix of a hundred strong directions over a floor of
+// 1e-3 ended 4e-2 off, coefficients whose curve is steep at 1 nowhere near.)
 // Matrices between products are images: part hi of all matrices, then part lo, rows padded to 32 bytes, under a power of two that comes from
 // the bounds of the singular values (step_factors(), for each matrix from its own norm: beside eps it may be tiny): entries stay below 2^15 and
 // far above the smallest half.  S and P are symmetric: only
@@ -515,7 +513,7 @@ struct Steps {
   int count;
   float c[3 * kMaxSteps];
 };
-// What the three products of each step multiply the sums and matrices of a matrix with: StepFactors, one float4 each.
+// What the three products of each step multiply with, for every matrix: StepFactors, a float4 each: of the sums; of S; of the diagonal.
 struct Factors {
   float4* at;
   int batch;
@@ -559,10 +557,10 @@ __global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, con
     const int i = (int)threadIdx.x;
     if (i < steps.count) {
       const float* const c = steps.c + 3 * i;
-      const StepFactors f = step_factors(s_most[i], grow(s_most[i], c[0], c[1], c[2], s_at[i]), c[0], c[1], c[2], i + 1 == steps.count, p.scale, std::is_same_v<O, __nv_bfloat16>);
+      const StepFactors f = step_factors(s_most[i], grow(s_most[i], c[0], c[1], c[2], s_at[i]), c[0], c[1], c[2], i + 1 == steps.count, p.scale);
       factors.of(i, 0)[blockIdx.y] = make_float4(f.gram, 0.f, 0.f, 0.f);
-      factors.of(i, 1)[blockIdx.y] = make_float4(f.square, f.linear, f.diagonal, f.unscale);
-      factors.of(i, 2)[blockIdx.y] = make_float4(f.move, f.own, 0.f, 0.f);
+      factors.of(i, 1)[blockIdx.y] = make_float4(f.square, f.linear, f.diagonal, 0.f);
+      factors.of(i, 2)[blockIdx.y] = make_float4(f.move, 0.f, 0.f, 0.f);
     }
     return;
   }
@@ -719,37 +717,33 @@ struct OrthogonalArgs {
   int* error_flag;
   int batch, rows, cols, k;     // of the products: D is rows x cols, the reduction has k steps
   const float4* factors;        // of every matrix, for this stage
-  Image s, to;                  // kPolynomial: S, kMove: X; where the result goes
-  const float* diagonals;       // 1 part, kPolynomial: of S (under its scale), kMove: a + those of P
-  float* to_diagonals;          // 1 part: where those of the result go
+  Image s, to;                  // kPolynomial: S; where the result goes
   void* out;                    // last kMove: the caller's matrix
   int out_type;
   long long ldo, stride_o;
   int boundary;                 // of its rows
 };
 
-template <Stage STAGE, int PARTS, int BN, bool A_MN, bool B_MN, bool PAIR>
+template <Stage STAGE, int BN, bool A_MN, bool B_MN>
 struct OrthogonalJob {
   using Args = OrthogonalArgs;
-  static constexpr int kParts = PARTS, kBN = BN;
-  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kTmaB = false, kTailed = false, kMeets = false, kPair = PAIR, kSymmetric = STAGE != kMove;
-  static constexpr int kTileRows = PAIR ? 2 * kBM : kBM, kBCols = PAIR ? BN / 2 : BN;
+  static constexpr int kParts = 2, kBN = BN;
+  static constexpr bool kAMn = A_MN, kBMn = B_MN, kTma = true, kTmaB = false, kTailed = false, kMeets = false, kPair = false, kSymmetric = STAGE != kMove;
   struct Item {
     int chunks, n, tail, matrix, row0, col0;
     bool turn;
   };
   const Args& a;
-  int rank;
-  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int rank_) : a(args), rank(rank_) {}
+  __device__ __forceinline__ OrthogonalJob(const Args& args, uint8_t*, int) : a(args) {}
   __device__ __forceinline__ bool bf16() const { return false; }
-  // pairs are for results that show where sums are cut (1000 x 767 in fp32: 4.7e-6 off with segments of 4 chunks, 1.4e-6 with one)
-  __device__ __forceinline__ int segment() const { return PARTS == 1 ? 16 : 2; }
+  // results show where sums are cut (1000 x 767 in fp32: 4.7e-6 off with segments of 4 chunks, 1.4e-6 with one)
+  __device__ __forceinline__ int segment() const { return 2; }
   __device__ __forceinline__ int* error_flag() const { return a.error_flag; }
   __device__ __forceinline__ void setup() {}
-  // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kTileRows / BN (i + 1)
+  // Tiles of a matrix: all, or for a symmetric one those of row block i whose columns do not lie behind it: kBM / BN (i + 1)
   __host__ __device__ static long long tiles(int rows, int cols) {
-    const long long m = (rows + kTileRows - 1) / kTileRows;
-    return kSymmetric ? kTileRows / BN * (m * (m + 1) / 2) : m * ((cols + BN - 1) / BN);
+    const long long m = (rows + kBM - 1) / kBM;
+    return kSymmetric ? kBM / BN * (m * (m + 1) / 2) : m * ((cols + BN - 1) / BN);
   }
   struct Walk {
     unsigned i, step;
@@ -763,8 +757,8 @@ struct OrthogonalJob {
     const unsigned t = i - (unsigned)it.matrix * per;
     unsigned row, col;
     if constexpr (kSymmetric) {
-      constexpr unsigned kAcross = kTileRows / BN;
-      const unsigned u = t / kAcross;   // in blocks of kTileRows columns
+      constexpr unsigned kAcross = kBM / BN;
+      const unsigned u = t / kAcross;   // in blocks of kBM columns
       row = (unsigned)((sqrtf(8.f * (float)u + 1.f) - 1.f) * 0.5f);
       while (row * (row + 1) / 2 > u) --row;
       while ((row + 1) * (row + 2) / 2 <= u) ++row;
@@ -775,8 +769,8 @@ struct OrthogonalJob {
       col = t - row * across;
     }
     it.col0 = (int)col * BN;
-    it.turn = kSymmetric && it.col0 + BN <= (int)row * kTileRows;
-    it.row0 = (int)row * kTileRows + rank * kBM;
+    it.turn = kSymmetric && it.col0 + BN <= (int)row * kBM;
+    it.row0 = (int)row * kBM;
     it.n = a.cols - it.col0;
     it.chunks = it.n > 0 ? (a.k + kBK - 1) / kBK : 0;   // (a symmetric matrix's last row block may reach past its columns)
     it.tail = kBK;
@@ -784,14 +778,14 @@ struct OrthogonalJob {
   }
   template <bool THERE>
   __device__ __forceinline__ void copy(const Item& it, int c, uint32_t tile, uint32_t bar) const {
-    constexpr int kBTile = kBCols * kBK * 2;
-    const int col0 = it.col0 + rank * kBCols;
-    const int boxes_a = A_MN ? min(kBM / 64, max(0, (a.rows - it.row0 + 63) / 64)) : kBM / 64, boxes_b = B_MN ? min(kBCols / 64, max(0, (a.cols - col0 + 63) / 64)) : kBCols / 64;
-    expect<THERE>(bar, (uint32_t)(PARTS * (boxes_a + boxes_b) * kGroup64));
+    constexpr int kBTile = BN * kBK * 2;
+    const int col0 = it.col0;
+    const int boxes_a = A_MN ? min(kBM / 64, max(0, (a.rows - it.row0 + 63) / 64)) : kBM / 64, boxes_b = B_MN ? min(BN / 64, max(0, (a.cols - col0 + 63) / 64)) : BN / 64;
+    expect<THERE>(bar, (uint32_t)(kParts * (boxes_a + boxes_b) * kGroup64));
 #pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
+    for (int part = 0; part < kParts; ++part) {
       const int z = part * a.batch + it.matrix;
-      const uint32_t ta = tile + part * kATile, tb = tile + PARTS * kATile + part * kBTile;
+      const uint32_t ta = tile + part * kATile, tb = tile + kParts * kATile + part * kBTile;
       if constexpr (A_MN) {
         for (int b = 0; b < boxes_a; ++b) copy_3d<THERE>(ta + b * kGroup64, &a.a, it.row0 + 64 * b, c * kBK, z, bar);
       } else {
@@ -806,10 +800,9 @@ struct OrthogonalJob {
   }
   // 32 elements of this lane's row of an image, two sectors of each part.  On their way while the columns before are worked on, the first while the
   // tile's products are formed.
-  static constexpr bool kReads = STAGE == kPolynomial || (STAGE == kMove && PARTS == 1);
-  __host__ __device__ static constexpr bool reads_low() { return PARTS == 2 ? STAGE == kPolynomial : STAGE == kMove; }
+  static constexpr bool kReads = STAGE == kPolynomial;
   struct Block {
-    uint32_t hi[16], lo[reads_low() ? 16 : 1];
+    uint32_t hi[16], lo[16];
   };
   struct Early : std::conditional_t<kReads, Block, Nothing> {
     float4 factors;   // of the matrix, on their way while its products are formed
@@ -820,13 +813,10 @@ struct OrthogonalJob {
     for (int h = 0; h < 2; ++h) {
       if (row < a.s.rows && col + 16 * h < a.s.ld) {
         load32(at + 16 * h, b.hi + 8 * h);
-        if constexpr (reads_low()) load32(at + 16 * h + a.s.part, b.lo + 8 * h);
+        load32(at + 16 * h + a.s.part, b.lo + 8 * h);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          b.hi[8 * h + e] = 0u;
-          if constexpr (reads_low()) b.lo[8 * h + e] = 0u;
-        }
+        for (int e = 0; e < 8; ++e) b.hi[8 * h + e] = b.lo[8 * h + e] = 0u;
       }
     }
   }
@@ -850,19 +840,8 @@ struct OrthogonalJob {
     const int rows_left = a.rows - row0, cols_left = a.cols - col0;
     if (rows_left <= 0 || cols_left <= 0) return;
     const float4 factors = next.factors;
-    // of the sums; of S or X; of the diagonal of P, and what takes its scale off
-    const float factor = factors.x, linear = factors.y, on_diagonal = factors.z, unscale = factors.w;
-    const bool diagonal = kSymmetric && row0 < col0 + NC && col0 < row0 + 32;   // whether the warp holds some of it
-    // 1 part: the diagonal entry of this lane's row, and those of the columns, NC / 32 a lane
-    constexpr bool kTall = STAGE == kMove && !B_MN;
-    const float* const d = PARTS == 1 && STAGE != kGram ? a.diagonals + (long long)it.matrix * (kTall ? a.cols : a.rows) : nullptr;
-    float mine = 0.f, theirs[NC / 32] = {};
-    if (PARTS == 1 && STAGE != kGram) {
-      if (!kTall) mine = d[min(row, a.rows - 1)];
-      if (STAGE == kPolynomial || kTall)
-#pragma unroll
-        for (int k = 0; k < NC / 32; ++k) theirs[k] = d[min(col0 + 32 * k + lane, a.cols - 1)];
-    }
+    const float factor = factors.x, linear = factors.y, on_diagonal = factors.z;
+    const bool diagonal = STAGE == kPolynomial && row0 < col0 + NC && col0 < row0 + 32;   // whether the warp holds some of it
     const bool out = STAGE == kMove && a.out != nullptr;
     const int out_size = a.out_type == kF32 ? 4 : 2;
     __half* const to = a.to.matrix(it.matrix);
@@ -878,35 +857,17 @@ struct OrthogonalJob {
         if constexpr (kReads) {
           const Block now = static_cast<const Block&>(next);
           if (c0 + 32 < NC) fetch(it, row, col0 + c0 + 32, next);
-          // of S b, with its diagonals apart b + c (D_i + D_j); of X the diagonal of P and a
-          const auto weight = [&](int c) {
-            if (STAGE == kPolynomial) return PARTS == 1 ? fmaf(factor, mine + __shfl_sync(0xffffffffu, theirs[c0 / 32], c), linear) : linear;
-            return (kTall ? __shfl_sync(0xffffffffu, theirs[c0 / 32], c) : mine) * linear;
-          };
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            float2 v = floats(now.hi[e]);
-            if constexpr (reads_low()) {
-              const float2 low = floats(now.lo[e]);
-              v = make_float2(fmaf(low.x, 0x1p-11f, v.x), fmaf(low.y, 0x1p-11f, v.y));
-            }
-            x[2 * e] = fmaf(weight(2 * e), v.x, x[2 * e]);
-            x[2 * e + 1] = fmaf(weight(2 * e + 1), v.y, x[2 * e + 1]);
+            const float2 v = floats(now.hi[e]), low = floats(now.lo[e]);
+            x[2 * e] = fmaf(linear, fmaf(low.x, 0x1p-11f, v.x), x[2 * e]);
+            x[2 * e + 1] = fmaf(linear, fmaf(low.y, 0x1p-11f, v.y), x[2 * e + 1]);
           }
         }
         if (diagonal) {
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            if (row == col0 + c0 + c) {
-              if constexpr (PARTS == 2) {
-                if (STAGE == kPolynomial) x[c] += on_diagonal;
-              } else {   // the image has none: O O alone is in x, b D + c D D is added
-                if (STAGE == kPolynomial) x[c] = fmaf(fmaf(fmaf(factor, mine, linear), mine, x[c]), unscale, on_diagonal);
-                if (row < a.rows) a.to_diagonals[(long long)it.matrix * a.rows + row] = x[c];
-                x[c] = 0.f;
-              }
-            }
-          }
+          for (int c = 0; c < 32; ++c)
+            if (row == col0 + c0 + c) x[c] += on_diagonal;
         }
         if (out && a.out_type == kF32) {
 #pragma unroll
@@ -923,17 +884,15 @@ struct OrthogonalJob {
           if (!out) {
             __half* const turned = to + (long long)(col0 + c0) * a.to.ld + row0;
             if (it.turn) put_turned(h, turned, a.to.ld, rows_left, cols_left - c0);
-            if constexpr (PARTS == 2 || STAGE == kMove) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float2 v = floats(h[e]);
-                h[e] = pack(kF16, (x[2 * e] - v.x) * 0x1p11f, (x[2 * e + 1] - v.y) * 0x1p11f);
-              }
-              RowStore lo_to = hi_to;
-              lo_to.out += 2 * a.to.part;
-              lo_to.put(c0, make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7]), make_uint4(h[8], h[9], h[10], h[11]), make_uint4(h[12], h[13], h[14], h[15]));
-              if (it.turn) put_turned(h, turned + a.to.part, a.to.ld, rows_left, cols_left - c0);
+            for (int e = 0; e < 16; ++e) {
+              const float2 v = floats(h[e]);
+              h[e] = pack(kF16, (x[2 * e] - v.x) * 0x1p11f, (x[2 * e + 1] - v.y) * 0x1p11f);
             }
+            RowStore lo_to = hi_to;
+            lo_to.out += 2 * a.to.part;
+            lo_to.put(c0, make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7]), make_uint4(h[8], h[9], h[10], h[11]), make_uint4(h[12], h[13], h[14], h[15]));
+            if (it.turn) put_turned(h, turned + a.to.part, a.to.ld, rows_left, cols_left - c0);
           }
         }
       }
@@ -1072,7 +1031,6 @@ std::size_t tickets_of(const ProductTn& p) { return 3ull * plan(p).grid; }
 struct OrthogonalSpace {
   double* partial;
   Image x[2], s, p;
-  float *s_diagonals, *p_diagonals;
   Factors factors;
   std::size_t bytes;
   OrthogonalSpace(const Orthogonal& o, void* space) {
@@ -1093,8 +1051,6 @@ struct OrthogonalSpace {
     x[1] = image(o.rows, o.cols);
     s = image(m, m);
     p = image(m, m);
-    s_diagonals = static_cast<float*>(take((std::size_t)o.batch * m * sizeof(float)));
-    p_diagonals = static_cast<float*>(take((std::size_t)o.batch * m * sizeof(float)));
     factors = Factors{static_cast<float4*>(take((std::size_t)o.steps * 3 * o.batch * sizeof(float4))), o.batch};
     bytes = used;
   }
@@ -1246,13 +1202,11 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
     e = launch_plain(k_start<decltype(in), decltype(out)>, dim3(start_blocks + 1, (unsigned)p.batch), room, p, vec, at.partial, partials,
                      p.steps > 0 ? at.x[0] : none, steps_of(p), at.factors);
   });
-  const bool halves = p.out_type == kBf16;   // one part is enough
   const auto map = [&](CUtensorMap* t, const Image& im, int cols, int box_rows) {
     return make_map(t, kF16, im.at, cols, im.rows, im.ld, 2LL * p.batch, (long long)im.rows * im.ld, box_rows);
   };
-  // Pairs of SMs where they all get a tile of 256 x 256, else the widest tile of 128 rows that every SM gets one of
-  const auto triangle = [&](int rows) { return p.batch * (cdiv(m, rows) * (cdiv(m, rows) + 1) / 2); };
-  const int bn = halves && triangle(256) >= kSms / 2 ? 256 : triangle(128) >= kSms ? 128 : 64;
+  // the widest tile that every SM gets one of
+  const int bn = p.batch * (cdiv(m, kBM) * (cdiv(m, kBM) + 1) / 2) >= kSms ? 128 : 64;
   for (int i = 0; i < p.steps && e == cudaSuccess; ++i) {
     const bool last = i + 1 == p.steps;
     const Image &x = at.x[i & 1], &y = at.x[(i + 1) & 1];
@@ -1262,27 +1216,22 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
       a.batch = p.batch;
       const long long items = J::tiles(a.rows, a.cols) * p.batch;
       if (items > INT_MAX) return cudaErrorInvalidValue;
-      return launch<J>(a, (unsigned)(J::kPair ? std::min<long long>(kSms, 2 * items) : std::min<long long>(kSms, items)), room);
+      return launch<J>(a, (unsigned)std::min<long long>(kSms, items), room);
     };
     OrthogonalArgs gram{}, poly{}, move{};
     gram.rows = gram.cols = m;
     gram.k = tall ? p.rows : p.cols;
     gram.factors = at.factors.of(i, 0);
     gram.to = at.s;
-    gram.to_diagonals = at.s_diagonals;
     poly.rows = poly.cols = poly.k = m;
     poly.factors = at.factors.of(i, 1);
     poly.s = at.s;
     poly.to = at.p;
-    poly.diagonals = at.s_diagonals;
-    poly.to_diagonals = at.p_diagonals;
     move.rows = p.rows;
     move.cols = p.cols;
     move.k = m;
     move.factors = at.factors.of(i, 2);
-    move.s = x;
     move.to = y;
-    move.diagonals = at.p_diagonals;
     if (last) {
       move.out = p.out;
       move.out_type = p.out_type;
@@ -1290,26 +1239,18 @@ cudaError_t enqueue(const Orthogonal& p, const Room& room) {
       move.stride_o = p.stride_o;
       move.boundary = boundary_of(p.out, p.ldo, p.batch > 1 ? p.stride_o : 0, size_of(p.out_type));
     }
-    const auto step = [&](auto parts, auto width) {
-      constexpr int PARTS = decltype(parts)::value, BN = decltype(width)::value;
-      constexpr bool PAIR = BN == 256;
-      constexpr int kRows = PAIR ? kBM : BN;   // of B that one block loads
-      const bool maps = map(&poly.a, at.s, m, kBM) && map(&poly.b, at.s, m, kRows) &&
-                        (tall ? map(&gram.a, x, p.cols, kBK) && map(&gram.b, x, p.cols, kBK) && map(&move.a, x, p.cols, kBM) && map(&move.b, at.p, m, kRows)
-                              : map(&gram.a, x, p.cols, kBM) && map(&gram.b, x, p.cols, kRows) && map(&move.a, at.p, m, kBM) && map(&move.b, x, p.cols, kBK));
+    const auto step = [&](auto width) {
+      constexpr int BN = decltype(width)::value;
+      const bool maps = map(&poly.a, at.s, m, kBM) && map(&poly.b, at.s, m, BN) &&
+                        (tall ? map(&gram.a, x, p.cols, kBK) && map(&gram.b, x, p.cols, kBK) && map(&move.a, x, p.cols, kBM) && map(&move.b, at.p, m, BN)
+                              : map(&gram.a, x, p.cols, kBM) && map(&gram.b, x, p.cols, BN) && map(&move.a, at.p, m, kBM) && map(&move.b, x, p.cols, kBK));
       if (!maps) return cudaErrorNotSupported;
-      cudaError_t q = tall ? product(Tag<OrthogonalJob<kGram, PARTS, BN, true, true, PAIR>>(), gram) : product(Tag<OrthogonalJob<kGram, PARTS, BN, false, false, PAIR>>(), gram);
-      if (q == cudaSuccess) q = product(Tag<OrthogonalJob<kPolynomial, PARTS, BN, false, false, PAIR>>(), poly);
-      if (q == cudaSuccess) q = tall ? product(Tag<OrthogonalJob<kMove, PARTS, BN, false, false, PAIR>>(), move) : product(Tag<OrthogonalJob<kMove, PARTS, BN, false, true, PAIR>>(), move);
+      cudaError_t q = tall ? product(Tag<OrthogonalJob<kGram, BN, true, true>>(), gram) : product(Tag<OrthogonalJob<kGram, BN, false, false>>(), gram);
+      if (q == cudaSuccess) q = product(Tag<OrthogonalJob<kPolynomial, BN, false, false>>(), poly);
+      if (q == cudaSuccess) q = tall ? product(Tag<OrthogonalJob<kMove, BN, false, false>>(), move) : product(Tag<OrthogonalJob<kMove, BN, false, true>>(), move);
       return q;
     };
-    const auto wide = [&](auto parts) {
-      if (bn == 64) return step(parts, std::integral_constant<int, 64>());
-      if constexpr (decltype(parts)::value == 1)
-        if (bn == 256) return step(parts, std::integral_constant<int, 256>());
-      return step(parts, std::integral_constant<int, 128>());
-    };
-    e = halves ? wide(std::integral_constant<int, 1>()) : wide(std::integral_constant<int, 2>());
+    e = bn == 64 ? step(std::integral_constant<int, 64>()) : step(std::integral_constant<int, 128>());
   }
   return e;
 }

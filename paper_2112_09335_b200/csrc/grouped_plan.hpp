@@ -156,21 +156,17 @@ GROUPED_BOTH double first_bound(double ratio) {
   if (frexp(ratio, &e) == 0.5) --e;
   return ldexp(1.0, e < kLeastBound ? kLeastBound : e);
 }
-// What the products of a step do beside multiplying: S = gram (X X^T), P = square (S S) + linear S + diagonal I, X' = move (P X) + own X.
+// What the products of a step do beside multiplying: S = gram (X X^T), P = square (S S) + linear S + diagonal I, X' = move (P X).
 struct StepFactors {
-  float gram;
-  float square, linear, diagonal, unscale;   // unscale: one over the scale of P
-  float move, own;                           // own: 1 part, beside the diagonals
+  float gram, square, linear, diagonal, move;
 };
 GROUPED_BOTH double bound_behind(const Growth& g) { return fmax(g.value, 0x1p-96); }
-// Of a step from a bound of `most` that grows by g.  `last`: the result leaves under `out_scale` instead of its own.  `halves`: the diagonal of P is kept
-// apart, without its scale.
-GROUPED_BOTH StepFactors step_factors(double most, const Growth& g, double a, double b, double c, bool last, double out_scale, bool halves) {
+// Of a step from a bound of `most` that grows by g.  `last`: the result leaves under `out_scale` instead of its own.
+GROUPED_BOTH StepFactors step_factors(double most, const Growth& g, double a, double b, double c, bool last, double out_scale) {
   const int x = scale_for(most), s = scale_for(most * most), p = scale_for(fmax(g.factor, 0x1p-400));
   const double out = last ? out_scale : 1.0;
   const int to = last ? 0 : scale_for(bound_behind(g));
-  return StepFactors{(float)ldexp(1.0, s - 2 * x), (float)ldexp(c, p - 2 * s), (float)ldexp(b, p - s), (float)(halves ? a : ldexp(a, p)),
-                     (float)ldexp(1.0, -p), (float)ldexp(out, to - p - x), (float)ldexp(out, to - x)};
+  return StepFactors{(float)ldexp(1.0, s - 2 * x), (float)ldexp(c, p - 2 * s), (float)ldexp(b, p - s), (float)ldexp(a, p), (float)ldexp(out, to - p - x)};
 }
 constexpr double kMostValue = 16.0, kMostFactor = 1024.0;
 

@@ -16,11 +16,11 @@ def ask(tmp_path_factory):
     exe = str(tmp_path_factory.mktemp("scales") / "harness")
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", os.path.join(HERE, "update_scales_harness.cpp"), "-o", exe], check=True)
 
-    def run(ratio, coefficients, halves=0, out_scale=1.0):
-        line = f"{ratio!r} {halves} {out_scale!r} {len(coefficients)} " + " ".join(repr(float(v)) for c in coefficients for v in c)
+    def run(ratio, coefficients, out_scale=1.0):
+        line = f"{ratio!r} {out_scale!r} {len(coefficients)} " + " ".join(repr(float(v)) for c in coefficients for v in c)
         got = [float(v) for v in subprocess.run([exe], input=line + "\n", capture_output=True, text=True, check=True).stdout.split()]
-        names = ("gram", "square", "linear", "diagonal", "unscale", "move", "own", "most")
-        return got[0], [dict(zip(names, got[1 + 8 * i:9 + 8 * i])) for i in range(len(coefficients))]
+        names = ("gram", "square", "linear", "diagonal", "move", "most")
+        return got[0], [dict(zip(names, got[1 + 6 * i:7 + 6 * i])) for i in range(len(coefficients))]
     return run
 
 
@@ -34,12 +34,11 @@ def test_the_first_bound_is_the_power_of_two_above(ask, ratio, first):
     assert ask(ratio, [])[0] == first
 
 
-@pytest.mark.parametrize("halves", [0, 1])
 @pytest.mark.parametrize("coefficients", [[MUON] * 5, [(1.5, -0.5, 0.0)] * 3, [(0.0, 1.25, 0.0)], [(0.0, 0.0, 1.0)], [(1e-9, 0.0, 0.0), MUON], [(0.0, 0.0, 1e-12)] * 2,
                                           [(0.0, 0.0, 0.0), MUON], [(2.0, -1.5, 0.5)] * 12])
-def test_scales_follow_the_bound_of_the_singular_values(ask, coefficients, halves):
+def test_scales_follow_the_bound_of_the_singular_values(ask, coefficients):
     for ratio in (1.0, 0.7, 1e-3, 1e-8, 1e-13, 1e-20, 1e-27):
-        first, steps = ask(ratio, coefficients, halves, 0.75)
+        first, steps = ask(ratio, coefficients, 0.75)
         s = np.linspace(0, ratio, 2001)
         assert first >= ratio
         before = first
@@ -49,16 +48,16 @@ def test_scales_follow_the_bound_of_the_singular_values(ask, coefficients, halve
             s = np.abs(s * (a + s**2 * (b + c * s**2)))
             assert s.max() <= f["most"] * (1 + 1e-12)
             assert all(math.isfinite(v) for v in f.values())
-            x, p = scale(before), 1.0 / f["unscale"] if f["unscale"] > 0 else math.inf
+            x = scale(before)
             to = 0.75 if i + 1 == len(coefficients) else scale(f["most"])
             assert f["gram"] == pytest.approx(scale(before**2) / x**2, rel=1e-7)
-            if factor > 0 and math.isfinite(p):
+            if factor > 0 and f["move"] > 0:
                 # P fills the halves: its bound lies in 2^14 .. 2^15 (a grid of 4001 points misses a maximum by less than 1e-5 of it)
+                p = 2.0 ** round(math.log2(to / (f["move"] * x)))
                 assert 2.0**14 * (1 - 1e-12) <= factor * p * (1 + 1e-5) and factor * p < 2.0**15 * (1 + 1e-5)
                 assert f["move"] == pytest.approx(to / (p * x), rel=1e-6)
-                assert f["diagonal"] == pytest.approx(a if halves else a * p, rel=1e-6)
+                assert f["diagonal"] == pytest.approx(a * p, rel=1e-6)
                 # what is left of a coefficient that falls out of fp32 is nothing beside the others: its share of P is below 2^-126 of the whole
                 assert f["linear"] == pytest.approx(b * p / scale(before**2), rel=1e-6, abs=2.0**-126)
                 assert f["square"] == pytest.approx(c * p / scale(before**2) ** 2, rel=1e-6, abs=2.0**-126)
-            assert f["own"] == pytest.approx(to / x, rel=1e-6)
             before = f["most"]
