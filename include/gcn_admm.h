@@ -184,9 +184,12 @@ int gcn_admm_dense_product_tn(gcn_admm* h, const float* A, const float* B, float
  * (No counterpart in the paper: the products of Problem 1 and of the block updates, for programs that give every group of rows a
  * weight of its own -- a weight per community of Section 2, or the experts of a layer whose rows were sorted by expert.)
  * Matrices are row-major on the handle's device, of `type`:
- *  GCN_ADMM_F32   products to fp32 accuracy: operands as sums of three bf16 numbers (24 bits, the exponents of fp32)
- *  GCN_ADMM_BF16, GCN_ADMM_F16   products exact, sums in fp32
- * Sums are rounded once, to out_type: the type of the operands, or GCN_ADMM_F32.  Leading dimensions and strides between matrices count
+ *  GCN_ADMM_F32   products to fp32 accuracy: operands as sums of three bf16 numbers (24 bits, the exponents of fp32; elements below 2^-110 are cut to
+ *                 multiples of 2^-133, the last bit of a bf16), of whose products those below 2^-21 of the whole are left out
+ *  GCN_ADMM_BF16, GCN_ADMM_F16   products exact
+ * Sums are formed in fp32, by tensor cores that cut them toward zero (a sum of K products is off by at most (37 + K / 512) 2^-23 of the sum of
+ * magnitudes where the result is fp32, (129 + K / 2048) 2^-23 where it has 16 bits), and rounded once, to out_type: the type of the operands, or
+ * GCN_ADMM_F32.  Leading dimensions and strides between matrices count
  * elements; 0 means dense.  Any alignment to whole elements and any sizes will do; 16-bit matrices whose address, leading dimension
  * and stride are multiples of 16 bytes are read fastest.  Infinite or NaN elements leave every result non-finite that the
  * formula has them in, though not always the same infinity or NaN; other results are untouched by them.

@@ -18,8 +18,8 @@
 // Operands have kParts parts of 16 bits:
 //   1   the operand itself
 //   2   x = hi + 2^-11 lo, halves (orthogonalised updates: entries bounded, a scale for every matrix)
-//   3   x = b0 + b1 + b2, bf16, each part what the last ones leave, cut after 8 bits: 24 bits in all, so the sum is x exactly, with the
-//       exponents of fp32 (no scales to keep, nothing for one large element to drown).  Products: b0 b0 and, apart, b0 b1 + b1 b0 + b1 b1 + b0 b2 + b2 b0;
+//   3   x = b0 + b1 + b2, bf16, each part what the last ones leave, cut after 8 bits: 24 bits in all, with the exponents of fp32 (no scales to
+//       keep, nothing for one large element to drown): the sum is x exactly from 2^-110 on; below, parts end at 2^-133, the last bit of a bf16.  Products: b0 b0 and, apart, b0 b1 + b1 b0 + b1 b1 + b0 b2 + b2 b0;
 //       what is left out is below 2^-21 of |x||y|, 2^-24 in the mean.
 // The main product and the corrections have accumulators of their own.  The tensor core cuts an accumulator toward zero at every
 // instruction; an error that grows with the length of the reduction is kept out by taking the accumulator into registers after

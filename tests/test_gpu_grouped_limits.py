@@ -103,3 +103,31 @@ def test_coefficients_that_make_everything_small(h, out, rows, cols):  # noqa: F
             continue
         rel = float((x.double() - want).norm() / want.norm())
         assert rel < ortho_tolerance(g, coefficients, x.dtype), (coefficients, rel)
+
+
+@pytest.mark.parametrize("rows", [90, 900])     # weights split tile by tile, and once for all tiles
+@pytest.mark.parametrize("ex, ew", [(-108, 0), (-112, 0), (-120, 0), (-130, 0), (-140, 3), (-120, 100), (-130, 120), (0, -125), (-60, -60)])
+def test_fp32_elements_near_the_end_of_their_range(h, rows, ex, ew):  # noqa: F811
+    """Parts of an fp32 element end at the last bit of a bf16, 2^-133: elements from 2^-110 on are exact sums of theirs, smaller ones are cut there, so that every
+    product with one is off by less than 2^-133 of the other factor.  Beyond that the usual tolerance."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    k, n = 96, 40
+
+    def made(e, *shape):
+        return (torch.randn(*shape, generator=gen, device="cuda", dtype=torch.float64) * 2.0**e).float()
+    x, w, d = made(ex, rows, k), made(ew, 1, k, n), made(ew, rows, n)
+    off = offsets_of([rows])
+    cut = lambda a: (a.double().abs() < 2.0**-110).double() * 2.0**-133      # noqa: E731
+    for transposed in (False, True):
+        v = w.mT.contiguous() if transposed else w
+        y = torch.empty(rows, n, device="cuda")
+        h.grouped_product(x.data_ptr(), v.data_ptr(), y.data_ptr(), off.data_ptr(), 1, rows, k, n, transpose_w=transposed)
+        a, b = x.double(), w[0].double()
+        lim = bound(y, a @ b, a.abs() @ b.abs(), k) + cut(x) @ b.abs() + a.abs() @ cut(w[0])
+        assert not bool(((y.double() - a @ b).abs() > lim).any())
+    dw = torch.empty(k, n, device="cuda")
+    h.grouped_product_tn(x.data_ptr(), d.data_ptr(), dw.data_ptr(), off.data_ptr(), 1, rows, k, n)
+    a, b = x.double().T, d.double()
+    lim = bound(dw, a @ b, a.abs() @ b.abs(), rows) + cut(x).T @ b.abs() + a.abs() @ cut(d)
+    assert not bool(((dw.double() - a @ b).abs() > lim).any())
