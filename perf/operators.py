@@ -120,6 +120,14 @@ def _counts(case, gen):
 
 
 def prepare(case, seed):
+    """Inputs, and where ``own`` is true the handle of the current device and stream: passes are enqueued on the stream that was current here."""
+    state = _inputs(case, seed)
+    if own:
+        state["handle"] = _trainer(torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream)
+    return state
+
+
+def _inputs(case, seed):
     gen = torch.Generator(device="cuda").manual_seed(1000003 * seed + 17)
     kind, out = TYPES[case["type"]], TYPES[case["out"]]
 
@@ -154,20 +162,20 @@ def prepare(case, seed):
 
 # ---- one pass --------------------------------------------------------------------------------------
 
-@functools.lru_cache(maxsize=1)
-def _trainer():
-    """The handle that a program keeps: its stream and workspace serve the calls."""
+@functools.lru_cache(maxsize=None)
+def _trainer(device, stream):
+    """The handle that a program keeps for a device and a stream: its workspace serves the calls."""
     import numpy as np
 
     from paper_2112_09335_b200 import binding
     one = np.ones((2, 1), dtype=np.float32)
-    return binding.GcnAdmm(2, np.array([0, 1, 2]), np.array([1, 0]), one, np.zeros(2), np.ones(2), [1, 1], 1, np.zeros(2), [one[:1]],
-                           stream=torch.cuda.current_stream().cuda_stream)
+    return binding.GcnAdmm(2, np.array([0, 1, 2]), np.array([1, 0]), one, np.zeros(2), np.ones(2), [1, 1], 1, np.zeros(2), [one[:1]], stream=stream,
+                           device=device)
 
 
 def _own(state):
     from paper_2112_09335_b200 import binding
-    case, out, h = state["case"], state["out"], _trainer()
+    case, out, h = state["case"], state["out"], state["handle"]
     types = dict(type=getattr(binding, case["type"].upper()), out_type=getattr(binding, case["out"].upper()))
     if case["path"] == "orthogonal":
         h.orthogonalise(state["g"].data_ptr(), out.data_ptr(), case["batch"], case["rows"], case["cols"], coefficients=[COEFFICIENTS] * case["steps"],
@@ -230,7 +238,7 @@ def run(state):
 # ---- the definition in 64 bits ---------------------------------------------------------------------
 
 def exact(case, seed):
-    state = prepare(case, seed)
+    state = _inputs(case, seed)
     if case["path"] == "orthogonal":
         a, b, c = COEFFICIENTS
         made = []
