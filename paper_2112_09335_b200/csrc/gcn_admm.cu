@@ -218,6 +218,7 @@ struct gcn_admm {
   int* d_comm_ptr = nullptr;              // [M+1] rows of the communities: the groups of a grouped product that names none
   gcn_admm_mem::Slab work;                // workspace of the grouped products and orthogonalised updates, counters of finished tiles first
   size_t work_tickets = 0;                // how many
+  size_t no_room_for = SIZE_MAX;          // least bytes of split weights that could not be had
   std::vector<std::pair<gcn_admm_mem::Slab, size_t>> old_work;   // what it was before it grew, and its counters: graphs that the caller captured still use it
   unsigned char* d_train = nullptr;
   int* d_train_rows = nullptr;            // new ids of the training rows, ascending
@@ -1968,14 +1969,18 @@ int gcn_admm_grouped_product(gcn_admm* h, int type, const void* x, long long ldx
     if (rows == 0) return;
     h->need_device({x, w, y, offsets});
     const gcn_admm_grouped::Room room = [&] {
+      const size_t images = gcn_admm_grouped::space_bytes(p);
       try {
-        return h->room_for(gcn_admm_grouped::space_bytes(p), 0);
+        return h->room_for(images, 0);
       } catch (const Fail& f) {
-        if (f.code != GCN_ADMM_ERR_ALLOC) throw;
+        // the images are for speed only: the same results, bit for bit, come without them.  (What was made once
+        // without them may be captured so: there room_for refuses to grow.)
+        if (f.code == GCN_ADMM_ERR_ALLOC) h->no_room_for = std::min(h->no_room_for, images);
+        else if (f.code != GCN_ADMM_ERR_ARG || images < h->no_room_for) throw;
         cudaGetLastError();
-        p.unsplit = true;   // the images are for speed only: the same results, bit for bit, come without them
-        return h->room_for(gcn_admm_grouped::space_bytes(p), 0);
+        p.unsplit = true;
       }
+      return h->room_for(gcn_admm_grouped::space_bytes(p), 0);
     }();
     char name[48];
     std::snprintf(name, sizeof name, "grouped@%dx%d", k, n);

@@ -39,16 +39,26 @@ def test_fp32_products_without_room_for_split_weights():
     w = torch.empty(groups, k, n, device="cuda").normal_(generator=gen)
     y = [torch.zeros(rows, n, device="cuda") for _ in range(2)]
     off = offsets_of([300] * 6 + [0, 300])
-    images, hog = 3 * groups * k * n * 2, None
+    images, hog, s = 3 * groups * k * n * 2, None, torch.cuda.Stream()
+    y.append(torch.zeros(rows, n, device="cuda"))
+    torch.cuda.synchronize()
     try:
         for i in range(2):
-            g = trainer()
+            g = trainer(stream=s.cuda_stream)
+            call = lambda to: g.grouped_product(x.data_ptr(), w.data_ptr(), to.data_ptr(), off.data_ptr(), groups, rows, k, n)  # noqa: B023, E731
             try:
                 if i == 1:      # memory for half of them is left
                     torch.cuda.empty_cache()
                     hog = torch.empty(torch.cuda.mem_get_info()[0] - images // 2, dtype=torch.uint8, device="cuda")
                     assert torch.cuda.mem_get_info()[0] < images
-                g.grouped_product(x.data_ptr(), w.data_ptr(), y[i].data_ptr(), off.data_ptr(), groups, rows, k, n)
+                call(y[i])
+                if i == 1:      # having been made once, the call may be captured
+                    graph = torch.cuda.CUDAGraph()
+                    with torch.cuda.graph(graph, stream=s, capture_error_mode="thread_local"):
+                        call(y[2])
+                    graph.replay()
+                    torch.cuda.synchronize()
+                    del graph
                 torch.cuda.synchronize()
             finally:
                 g.destroy()
@@ -58,7 +68,7 @@ def test_fp32_products_without_room_for_split_weights():
         torch.cuda.empty_cache()
     a, b = x[:300].double(), w[0, :, :200].double()
     assert not bool(((y[0][:300, :200].double() - a @ b).abs() > bound(y[0][:300, :200], a @ b, a.abs() @ b.abs(), k)).any())
-    assert torch.equal(y[0], y[1])
+    assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2])
 
 
 def orthogonalised(h, g, coefficients, eps, scale, out):  # noqa: F811
