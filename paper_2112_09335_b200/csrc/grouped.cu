@@ -513,7 +513,7 @@ struct Steps {
   int count;
   float c[3 * kMaxSteps];
 };
-// What the three products of each step multiply with, for every matrix: StepFactors, a float4 each: of the sums; of S; of the diagonal.
+// What the three products of each step multiply with, for every matrix: StepFactors, a float4 each: of the sums; of S (X: of the result); of the diagonal.
 struct Factors {
   float4* at;
   int batch;
@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(256) k_start(const Orthogonal p, bool vec, con
       const StepFactors f = step_factors(s_most[i], grow(s_most[i], c[0], c[1], c[2], s_at[i]), c[0], c[1], c[2], i + 1 == steps.count, p.scale);
       factors.of(i, 0)[blockIdx.y] = make_float4(f.gram, 0.f, 0.f, 0.f);
       factors.of(i, 1)[blockIdx.y] = make_float4(f.square, f.linear, f.diagonal, 0.f);
-      factors.of(i, 2)[blockIdx.y] = make_float4(f.move, 0.f, 0.f, 0.f);
+      factors.of(i, 2)[blockIdx.y] = make_float4(f.move, f.scale, 0.f, 0.f);
     }
     return;
   }
@@ -853,7 +853,7 @@ struct OrthogonalJob {
       if (c0 < cols_left) {
         float x[32];
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = acc[c0 + c] * factor;
+        for (int c = 0; c < 32; ++c) x[c] = STAGE == kMove ? acc[c0 + c] * factor * linear : acc[c0 + c] * factor;
         if constexpr (kReads) {
           const Block now = static_cast<const Block&>(next);
           if (c0 + 32 < NC) fetch(it, row, col0 + c0 + 32, next);

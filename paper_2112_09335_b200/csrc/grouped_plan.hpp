@@ -156,17 +156,18 @@ GROUPED_BOTH double first_bound(double ratio) {
   if (frexp(ratio, &e) == 0.5) --e;
   return ldexp(1.0, e < kLeastBound ? kLeastBound : e);
 }
-// What the products of a step do beside multiplying: S = gram (X X^T), P = square (S S) + linear S + diagonal I, X' = move (P X).
+// What the products of a step do beside multiplying: S = gram (X X^T), P = square (S S) + linear S + diagonal I, X' = scale (move (P X)); `scale` is
+// the caller's in the last step, apart because move may be so small that with it fp32 would end.
 struct StepFactors {
-  float gram, square, linear, diagonal, move;
+  float gram, square, linear, diagonal, move, scale;
 };
 GROUPED_BOTH double bound_behind(const Growth& g) { return fmax(g.value, 0x1p-96); }
-// Of a step from a bound of `most` that grows by g.  `last`: the result leaves under `out_scale` instead of its own.
-GROUPED_BOTH StepFactors step_factors(double most, const Growth& g, double a, double b, double c, bool last, double out_scale) {
+// Of a step from a bound of `most` that grows by g.  `last`: the result leaves under `out_scale` instead of one of its own.
+GROUPED_BOTH StepFactors step_factors(double most, const Growth& g, double a, double b, double c, bool last, float out_scale) {
   const int x = scale_for(most), s = scale_for(most * most), p = scale_for(fmax(g.factor, 0x1p-400));
-  const double out = last ? out_scale : 1.0;
   const int to = last ? 0 : scale_for(bound_behind(g));
-  return StepFactors{(float)ldexp(1.0, s - 2 * x), (float)ldexp(c, p - 2 * s), (float)ldexp(b, p - s), (float)ldexp(a, p), (float)ldexp(out, to - p - x)};
+  return StepFactors{(float)ldexp(1.0, s - 2 * x), (float)ldexp(c, p - 2 * s), (float)ldexp(b, p - s), (float)ldexp(a, p), (float)ldexp(1.0, to - p - x),
+                     last ? out_scale : 1.f};
 }
 constexpr double kMostValue = 16.0, kMostFactor = 1024.0;
 

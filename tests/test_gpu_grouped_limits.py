@@ -141,3 +141,14 @@ def test_fp32_elements_near_the_end_of_their_range(h, rows, ex, ew):  # noqa: F8
     a, b = x.double().T, d.double()
     lim = bound(dw, a @ b, a.abs() @ b.abs(), rows) + cut(x).T @ b.abs() + a.abs() @ cut(d)
     assert not bool(((dw.double() - a @ b).abs() > lim).any())
+
+
+@pytest.mark.parametrize("scale", [1e-33, -3e-30, 1e30])
+@pytest.mark.parametrize("rows, cols", SMALL)
+def test_scales_near_the_ends_of_fp32(h, scale, rows, cols):  # noqa: F811
+    import torch
+    g = torch.randn(2, rows, cols, generator=torch.Generator(device="cuda").manual_seed(cols), device="cuda")
+    for coefficients in ([MUON] * 5, [(0.5, 0.0, 0.0)], []):
+        x = orthogonalised(h, g, coefficients, 1e-7, scale, "f32")
+        want = newton_schulz(g, coefficients, 1e-7, scale)
+        assert float((x.double() - want).norm() / want.norm()) < ortho_tolerance(g, coefficients, x.dtype), coefficients

@@ -19,8 +19,8 @@ def ask(tmp_path_factory):
     def run(ratio, coefficients, out_scale=1.0):
         line = f"{ratio!r} {out_scale!r} {len(coefficients)} " + " ".join(repr(float(v)) for c in coefficients for v in c)
         got = [float(v) for v in subprocess.run([exe], input=line + "\n", capture_output=True, text=True, check=True).stdout.split()]
-        names = ("gram", "square", "linear", "diagonal", "move", "most")
-        return got[0], [dict(zip(names, got[1 + 6 * i:7 + 6 * i])) for i in range(len(coefficients))]
+        names = ("gram", "square", "linear", "diagonal", "move", "scale", "most")
+        return got[0], [dict(zip(names, got[1 + 7 * i:8 + 7 * i])) for i in range(len(coefficients))]
     return run
 
 
@@ -49,7 +49,8 @@ def test_scales_follow_the_bound_of_the_singular_values(ask, coefficients):
             assert s.max() <= f["most"] * (1 + 1e-12)
             assert all(math.isfinite(v) for v in f.values())
             x = scale(before)
-            to = 0.75 if i + 1 == len(coefficients) else scale(f["most"])
+            to = 1.0 if i + 1 == len(coefficients) else scale(f["most"])
+            assert f["scale"] == (0.75 if i + 1 == len(coefficients) else 1.0)
             assert f["gram"] == pytest.approx(scale(before**2) / x**2, rel=1e-7)
             if factor > 0 and f["move"] > 0:
                 # P fills the halves: its bound lies in 2^14 .. 2^15 (a grid of 4001 points misses a maximum by less than 1e-5 of it)

@@ -25,7 +25,7 @@ int main() {
       const Growth g = grow(most, a, b, c);
       const StepFactors f = step_factors(most, g, a, b, c, i + 1 == steps, out_scale);
       most = bound_behind(g);
-      std::printf(" %.9g %.9g %.9g %.9g %.9g %.17g", f.gram, f.square, f.linear, f.diagonal, f.move, most);
+      std::printf(" %.9g %.9g %.9g %.9g %.9g %.9g %.17g", f.gram, f.square, f.linear, f.diagonal, f.move, f.scale, most);
     }
     std::printf("\n");
   }
