@@ -14,9 +14,10 @@ namespace gcn_admm_grouped {
 // hold them.  Only words with a valid half may be loaded: where there is none, the address itself may lie anywhere.
 struct HalfWords {
   std::uintptr_t first;   // address of word 0
-  int odd, some;          // whether the first half is the second of its word; halves that are valid
-  GROUPED_BOTH HalfWords(std::uintptr_t address, int valid) : first(address & ~std::uintptr_t(3)), odd((int)(address >> 1 & 1)), some(valid < 0 ? 0 : valid > 8 ? 8 : valid) {}
-  GROUPED_BOTH bool holds(int word) const { return some > 0 && 2 * word < some + odd; }
+  int some, odd;          // halves that are valid; whether the first of them is the second of its word
+  GROUPED_BOTH HalfWords(std::uintptr_t address, int valid)
+      : first(address & ~std::uintptr_t(3)), some(valid < 0 ? 0 : valid > 8 ? 8 : valid), odd(valid > 0 ? (int)(address >> 1 & 1) : 0) {}
+  GROUPED_BOTH bool holds(int word) const { return 2 * word < some + odd; }
 };
 
 // Byte offset of part k of an element whose parts lie `apart` bytes from each other (images of split weights are longer than an int counts).
