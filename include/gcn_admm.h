@@ -188,19 +188,21 @@ int gcn_admm_dense_product_tn(gcn_admm* h, const float* A, const float* B, float
  *                 multiples of 2^-133, the last bit of a bf16), of whose products those below 2^-21 of the whole are left out
  *  GCN_ADMM_BF16, GCN_ADMM_F16   products exact
  * Sums are formed in fp32, by tensor cores that cut them toward zero (a sum of K products is off by at most (37 + K / 512) 2^-23 of the sum of
- * magnitudes where the result is fp32, (129 + K / 2048) 2^-23 where it has 16 bits), and rounded once, to out_type: the type of the operands, or
- * GCN_ADMM_F32.  Leading dimensions and strides between matrices count
- * elements; 0 means dense.  Any alignment to whole elements and any sizes will do; 16-bit matrices whose address, leading dimension
- * and stride are multiples of 16 bytes are read fastest.  Infinite or NaN elements leave every result non-finite that the
- * formula has them in, though not always the same infinity or NaN; other results are untouched by them.
+ * magnitudes where the result is fp32, (129 + K / 2048) 2^-23 where it has 16 bits), and rounded once, to out_type: the type of the
+ * operands, or GCN_ADMM_F32.  Leading dimensions and strides between matrices count elements; 0 means dense.  Any alignment to whole
+ * elements and any sizes will do; 16-bit matrices whose address, leading dimension and stride are multiples of 16 bytes are read
+ * fastest.  Infinite or NaN elements leave every result non-finite that the formula has them in, though not always the same infinity or
+ * NaN; other results are untouched by them.
  * Group g owns the rows offsets[g] <= i < offsets[g+1], 0 <= g < n_groups <= 1024, cut to 0..rows; where offsets descend it
  * owns none.  offsets: device array of n_groups + 1 ints, read when the work runs, so that a router on the device may write them.  NULL: the
  * handle's communities, in the order of gcn_admm_index (n_groups and rows must then be the handle's).  Groups should not overlap (rows of two
  * groups get one of the two results).  Results may not alias operands.
  * All work is enqueued on the handle's stream; the calls return without synchronising, may be captured, and give the same bits
- * every time.  gcn_admm_grouped_product (fp32, many rows: its weights as three parts; where there is no memory for them every tile splits its own, slower and with the same bits), gcn_admm_grouped_product_tn and
- * gcn_admm_orthogonalise use a workspace of the handle that grows when a call needs more of it: the first call of a size allocates and may not be
- * part of a capture (it is refused there); what it was before stays with the handle, for graphs that hold it.  Calls, and replays of captured ones, that share a handle must follow one another on its stream.  A bounded wait that runs out on the device is reported like that of any product (see
+ * every time.  gcn_admm_grouped_product (fp32, many rows: its weights as three parts; where there is no memory for them every tile
+ * splits its own, slower and with the same bits), gcn_admm_grouped_product_tn and gcn_admm_orthogonalise use a workspace of the handle
+ * that grows when a call needs more of it: the first call of a size allocates and may not be part of a capture (it is refused there);
+ * what it was before stays with the handle, for graphs that hold it.  Calls, and replays of captured ones, that share a handle must follow
+ * one another on its stream.  A bounded wait that runs out on the device is reported like that of any product (see
  * GCN_ADMM_ST_PIPELINE_FLAG). */
 enum { GCN_ADMM_F32 = 0, GCN_ADMM_BF16 = 1, GCN_ADMM_F16 = 2 };
 
@@ -221,9 +223,11 @@ int gcn_admm_grouped_product_tn(gcn_admm* h, int type, const void* x, long long 
  * `batch` matrices G, rows x cols, X_0 = G / (||G||_F + eps) and n_steps times X <- a X + (b A + c A A) X with A = X X^T (X^T in place
  * of X where rows > cols); out = scale X.  coefficients: a, b, c of every step, host array of 3 n_steps floats.  Each singular value s
  * goes to s (a + b s^2 + c s^4); coefficients that let one grow above 16, or a factor a + b s^2 + c s^4 above 1024, are refused.  A
- * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  Results of every type come from products to fp32 accuracy, by
- * pairs of halves under scales of each matrix (its entries are bounded by its singular values, which start from at most ||G|| / (||G|| + eps): a matrix
- * whose norm is far below eps is as accurate as any, down to 2^-96 of it), and are rounded once.  out may be g itself, with the same type and strides. */
+ * zero matrix stays zero; a matrix with an infinite or NaN element becomes NaN.  Results of every type come
+ * from products to fp32 accuracy, by pairs of halves (22 bits) under scales of each matrix (its entries are bounded by its singular values,
+ * which start from at most ||G|| / (||G|| + eps): a matrix whose norm is far below eps is as accurate as any, down to 2^-96 of it), and are
+ * rounded once.  Steps lift small singular values, and what they are off, as in any arithmetic of 32 bits.  out may be g itself, with the
+ * same type and strides. */
 int gcn_admm_orthogonalise(gcn_admm* h, int type, int batch, int rows, int cols, const void* g, long long ldg, long long stride_g,
                            int n_steps, const float* coefficients, float eps, float scale, int out_type, void* out, long long ldo,
                            long long stride_o);

@@ -240,7 +240,9 @@ struct ProductJob {
 // Tiles of groups of unequal length do not share out evenly.  Workers (blocks, or pairs of blocks) take whole tiles in turn while
 // there is more than one round of them left (all of them, from kWholeRounds on), so that those at work at the same time read the same group's rows; what remains, up to two rounds, is seen as one
 // stretch of chunks (group, tile, chunk of rows in this order), of which every worker gets what brings it to the mean.  So few
-// tiles still fill the chip, and no long group is walked by one worker while the others wait.  (169343 x 256 x 40 in 32 groups, 64 tiles: 143 us in
+// tiles still fill the chip, and with fewer than kWholeRounds rounds a long group is not walked by one worker while the others wait.  From there on tiles are dealt by
+// their number alone: a group far longer than the others keeps the workers of its tiles (600 groups of 64 x 64, one of 150000 rows and the others of ten: 810 us;
+// as many rows in equal groups: 20).  (169343 x 256 x 40 in 32 groups, 64 tiles: 143 us in
 // pieces of a length fixed beforehand, 88 us so; all work as one stretch took 259 us for 16384 x 2048 x 1024 in 16 groups, where each worker read rows of its
 // own, instead of 118.)
 // A tile that several workers share is put together from their sums, which they leave in the workspace: whoever comes last of up

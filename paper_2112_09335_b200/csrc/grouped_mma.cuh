@@ -19,8 +19,9 @@
 //   1   the operand itself
 //   2   x = hi + 2^-11 lo, halves (orthogonalised updates: entries bounded, a scale for every matrix)
 //   3   x = b0 + b1 + b2, bf16, each part what the last ones leave, cut after 8 bits: 24 bits in all, with the exponents of fp32 (no scales to
-//       keep, nothing for one large element to drown): the sum is x exactly from 2^-110 on; below, parts end at 2^-133, the last bit of a bf16.  Products: b0 b0 and, apart, b0 b1 + b1 b0 + b1 b1 + b0 b2 + b2 b0;
-//       what is left out is below 2^-21 of |x||y|, 2^-24 in the mean.
+//       keep, nothing for one large element to drown): the sum is x exactly from 2^-110 on; below, parts end at 2^-133, the last bit of a bf16.
+//       Products: b0 b0 and, apart, b0 b1 + b1 b0 + b1 b1 + b0 b2 + b2 b0; what is left out, b1 b2 + b2 b1 and b2 b2, has the sign of the product and is
+//       below 2^-21 of |x||y|, 2^-24 in the mean.
 // The main product and the corrections have accumulators of their own.  The tensor core cuts an accumulator toward zero at every
 // instruction; an error that grows with the length of the reduction is kept out by taking the accumulator into registers after
 // every segment of 256 steps or fewer (1024 where a result of 16 bits would not show it), where segments are added in fp32, rounded to nearest.  Two accumulators alternate, so that instructions of a segment run
@@ -169,8 +170,8 @@ struct Bars {
 // once.  Otherwise they go through a buffer in shared memory, so that what leaves a warp at once are 64 bytes of each of eight rows; where they
 // do not lie on 16-byte boundaries either, or end inside of 16 bytes, a warp writes 16 columns (fp32) or 32 of two rows at once, halves two by
 // two in whichever way they are aligned (13752 x 767 halves, with their product: 87 us where each lane wrote eight halves one by one, 42 us
-// so).  Neither
-// is kept in L1 (169343 x 128 x 256 fp32 103 -> 92 us, 4096 x 4096 updates 1.44 -> 1.28 ms).  The buffer is not for all: while a pair multiplies, its operands alone take 128 bytes a clock from and to shared memory, all there are.
+// so).  Whole
+// sectors are not kept in L1 (weight gradients of 16384 x 2048 x 1024 to fp32: 111 -> 101 us); what goes through the buffer leaves by ordinary stores.  The buffer is not for all: while a pair multiplies, its operands alone take 128 bytes a clock from and to shared memory, all there are.
 __device__ __forceinline__ void store32(void* at, const uint4& a, const uint4& b) {
   asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
