@@ -129,9 +129,10 @@ GROUPED_BOTH Stationary stationary(double a, double b, double c) {
     at.factor = step_factor(at.t, a, b, c);
   }
   const double d = 9.0 * b * b - 20.0 * a * c;   // of a + 3 b t + 5 c t^2
-  if (d >= 0.0) {
-    consider(0, (-3.0 * b + sqrt(d)) / (10.0 * c));
-    consider(1, (-3.0 * b - sqrt(d)) / (10.0 * c));
+  if (d >= 0.0) {   // its roots, without the difference that loses one of them where c is small
+    const double q = -0.5 * (3.0 * b + copysign(sqrt(d), b));
+    consider(0, q / (5.0 * c));
+    consider(1, a / q);
   }
   return at;
 }

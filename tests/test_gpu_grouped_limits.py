@@ -152,3 +152,15 @@ def test_scales_near_the_ends_of_fp32(h, scale, rows, cols):  # noqa: F811
         x = orthogonalised(h, g, coefficients, 1e-7, scale, "f32")
         want = newton_schulz(g, coefficients, 1e-7, scale)
         assert float((x.double() - want).norm() / want.norm()) < ortho_tolerance(g, coefficients, x.dtype), coefficients
+
+
+@pytest.mark.parametrize("coefficients", [[(3.9, -3.9, 1e-20)], [(2.0, -1.5, 1e-30), MUON], [(-3.9, 3.9, 1e-12)]])
+@pytest.mark.parametrize("rows, cols", SMALL)
+def test_coefficients_nearly_zero(h, coefficients, rows, cols):  # noqa: F811
+    """One strong direction beside weak ones: singular values all over 0 .. 1."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    g = torch.randn(1, rows, cols, generator=gen, device="cuda") * 0.05 + torch.randn(1, rows, 1, generator=gen, device="cuda") @ torch.randn(1, 1, cols, generator=gen, device="cuda")
+    x = orthogonalised(h, g, coefficients, 1e-7, 1.0, "f32")
+    want = newton_schulz(g, coefficients, 1e-7, 1.0)
+    assert float((x.double() - want).norm() / want.norm()) < ortho_tolerance(g, coefficients, x.dtype)

@@ -62,3 +62,15 @@ def test_scales_follow_the_bound_of_the_singular_values(ask, coefficients):
                 assert f["linear"] == pytest.approx(b * p / scale(before**2), rel=1e-6, abs=2.0**-126)
                 assert f["square"] == pytest.approx(c * p / scale(before**2) ** 2, rel=1e-6, abs=2.0**-126)
             before = f["most"]
+
+
+@pytest.mark.parametrize("coefficients", [(3.9, -3.9, 1e-20), (2.0, -1.5, 1e-30), (3.0, -3.0, -1e-17), (-3.9, 3.9, 1e-12), (0.5, 0.0, -1e-25), (0.0, 2.0, -1.5), (0.0, 0.0, 1.0)])
+def test_bounds_hold_where_a_coefficient_is_nearly_zero(ask, coefficients):
+    """Stationary points are roots of a + 3 b t + 5 c t^2, one of which a difference of nearly equal numbers would lose."""
+    for ratio in (1.0, 0.8):
+        first, steps = ask(ratio, [coefficients])
+        s = np.linspace(0, first, 20001)
+        a, b, c = (float(np.float32(v)) for v in coefficients)
+        value = np.abs(s * (a + s**2 * (b + c * s**2))).max()
+        # the grid's steps are 5e-5 and second derivatives below 30: it misses a maximum by less than 30 (5e-5)^2 / 8
+        assert value <= steps[0]["most"] * (1 + 1e-12) and steps[0]["most"] <= value + 1e-8
