@@ -86,3 +86,18 @@ def test_updates_of_16_bits_are_those_of_fp32_rounded(h, kind, batch, rows, cols
     for i in range(batch):
         rel = float((y[i].double() - want[i]).norm() / want[i].norm())
         assert rel < ortho_tolerance(g[i:i + 1], coefficients, torch.float32), (i, rel)
+
+
+@pytest.mark.parametrize("k, n", [(7, 5), (64, 40), (100, 256), (129, 70), (331, 264)])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_fp32_weights_split_once_or_by_tile_give_the_same_bits(h, k, n, transposed):  # noqa: F811
+    """Two groups of 500 rows have their weights split once; with three idle groups more they are too few rows for that."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    x, w = torch.randn(1000, k, generator=gen, device="cuda"), torch.randn(5, *((n, k) if transposed else (k, n)), generator=gen, device="cuda")
+    y = [torch.zeros(1000, n, device="cuda") for _ in range(2)]
+    for i, sizes in enumerate(([500, 500], [500, 500, 0, 0, 0])):
+        off = offsets_of(sizes)
+        h.grouped_product(x.data_ptr(), w.data_ptr(), y[i].data_ptr(), off.data_ptr(), len(sizes), 1000, k, n, transpose_w=transposed)
+        torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1])
